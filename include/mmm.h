@@ -340,6 +340,82 @@ mmm_status mmm_matmul_static_scratch(const mmm_maps *maps, mmm_dtype dt,
                                      const void *X, int64_t ldx, const void *Y, int64_t ldy,
                                      void *C, int64_t ldc, int32_t accumulate, void *hip_stream);
 
+/* ---- The operators around the product, and their gradients.  Conventions as above.  Everything is computed in float and rounded to
+ * nearest even once, where it is written to a 16-bit type. */
+
+typedef enum {
+    MMM_ACT_NONE = 0,
+    MMM_ACT_RELU = 1,        /* max(z, 0); NaN stays NaN                                       */
+    MMM_ACT_GELU = 2,        /* z Phi(z), Phi the normal distribution function                 */
+    MMM_ACT_GELU_TANH = 3,   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2              */
+    MMM_ACT_SILU = 4         /* z / (1 + exp(-z))                                              */
+} mmm_activation;
+
+/* The gradient through the epilogue:
+ *     dZ[i,j] = dC[i,j] act'(Z[i,j])        dbias[j] = sum over i of dC[i,j] act'(Z[i,j])
+ * (that of the residual is dC itself).  dC and Z have out_dtype, dZ has dt; out_dtype is dt or MMM_F32; no doubles.  Z may be NULL without an
+ * activation.  dZ may be dC or Z itself (same type and leading dimension).  dZ or dbias (N floats) may be NULL.  dbias is summed
+ * in float, before dZ is rounded, in an order that depends on the shape only.
+ * workspace: 256-byte aligned device memory of mmm_epilogue_backward_workspace_bytes(), needed with dbias only; two
+ * calls that may run at the same time need one each.  Nothing in it has to be kept or cleared between calls.
+ * Errors: MMM_ERR_INVALID_ARG, MMM_ERR_SHAPE (M, N < 1 or above 2^30, leading dimension too small), MMM_ERR_DTYPE, MMM_ERR_WORKSPACE, MMM_ERR_DEVICE. */
+mmm_status mmm_epilogue_backward_workspace_bytes(int64_t M, int64_t N, size_t *bytes);
+mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype out_dtype, int32_t activation,
+                                 const void *dC, int64_t lddc, const void *Z, int64_t ldz, void *dZ, int64_t lddz,
+                                 float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The norms around a block.  For every row i of N elements:
+ *     v  = norm_post(y) * post_weight + post_bias          (post == MMM_NORM_NONE: v = y)
+ *     h' = alpha h + gate v                                (no block, y == NULL: h' = h)
+ *     n  = norm_pre(h') * pre_weight + pre_bias            (pre == MMM_NORM_NONE: no n)
+ * MMM_NORM_RMS: x / sqrt(mean(x^2) + eps); MMM_NORM_LAYER: (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps).  n is that of h' before it is
+ * rounded to its type. */
+typedef enum { MMM_NORM_NONE = 0, MMM_NORM_RMS = 1, MMM_NORM_LAYER = 2 } mmm_norm_kind;
+/* shape of the gate: one value per row, per column, or M x ldgate of them */
+typedef enum { MMM_GATE_NONE = 0, MMM_GATE_ROW = 1, MMM_GATE_COL = 2, MMM_GATE_FULL = 3 } mmm_gate_kind;
+#define MMM_NORM_MAX_WIDTH 32768
+typedef struct {
+    int64_t M, N;            /* rows; width, at most MMM_NORM_MAX_WIDTH                        */
+    int32_t dt;              /* mmm_dtype of n, gate, weights and biases (no doubles)          */
+    int32_t dt_h, dt_y;      /* of h, h' and of y: dt or MMM_F32                               */
+    int32_t post, pre;       /* mmm_norm_kind                                                  */
+    int32_t gate;            /* mmm_gate_kind                                                  */
+    float eps, alpha;        /* eps >= 0                                                       */
+} mmm_block_norm_desc;
+
+/* h and y are rows of ldh and ldy elements, h_out and n of ldh_out and ldn.  h_out may be NULL (not stored; there must be n then) or h itself
+ * (same leading dimension); with y == NULL it must be NULL.  Weights and biases (N elements each) are optional; they must be NULL
+ * where their norm is MMM_NORM_NONE.  gate_values must be given exactly where desc->gate says so; a gate and a norm behind the block need y.
+ * Outputs overlap nothing else.
+ * Errors: MMM_ERR_INVALID_ARG, MMM_ERR_SHAPE, MMM_ERR_DTYPE (type not allowed, misaligned pointer), MMM_ERR_DEVICE. */
+mmm_status mmm_block_norm(const mmm_block_norm_desc *desc, const void *h, int64_t ldh, const void *y, int64_t ldy,
+                          const void *gate_values, int64_t ldgate, const void *post_weight, const void *post_bias,
+                          const void *pre_weight, const void *pre_bias, void *h_out, int64_t ldh_out, void *n, int64_t ldn,
+                          void *hip_stream);
+
+/* Its gradients.  h_out is the h' of the forward call as stored (h where there was no block; needed with a norm in front, else NULL is allowed), d_n and d_h_out the
+ * gradients that come in (d_n must be given exactly where there is a norm in front; d_h_out == NULL: zero, which needs d_n).  Outputs, each optional:
+ *   d_h (dt_h), d_y (dt_y), d_gate (float for MMM_GATE_ROW and MMM_GATE_COL, M x ldd_gate of dt for MMM_GATE_FULL),
+ *   d_post_weight, d_post_bias, d_pre_weight, d_pre_bias (N floats each; the values the forward call had may be NULL, i.e. 1 and 0).
+ * d_h may be d_h_out itself (same leading dimension).  Sums over rows are float sums in an order that depends on the shape only.
+ * workspace as mmm_epilogue_backward's, of mmm_block_norm_backward_workspace_bytes(); needed where any sum over rows is asked for (d_gate of
+ * MMM_GATE_COL among them).  Errors: as mmm_block_norm, MMM_ERR_WORKSPACE. */
+typedef struct {
+    const void *h_out; int64_t ldh_out;
+    const void *y; int64_t ldy;
+    const void *gate_values; int64_t ldgate;
+    const void *post_weight, *post_bias, *pre_weight;
+    const void *d_n; int64_t ldd_n;
+    const void *d_h_out; int64_t ldd_h_out;
+    void *d_h; int64_t ldd_h;
+    void *d_y; int64_t ldd_y;
+    void *d_gate; int64_t ldd_gate;
+    float *d_post_weight, *d_post_bias, *d_pre_weight, *d_pre_bias;
+} mmm_block_norm_grads;
+mmm_status mmm_block_norm_backward_workspace_bytes(int64_t M, int64_t N, size_t *bytes);
+mmm_status mmm_block_norm_backward(const mmm_block_norm_desc *desc, const mmm_block_norm_grads *grads, void *workspace,
+                                   size_t workspace_bytes, void *hip_stream);
+
 /* Process-wide tuning knobs (for benchmarking; the defaults choose by shape).
  *   "matmul_variant": -1 = automatic, else index of a compiled tile variant
  *   "split_k"       :  0 = automatic, else the number of K splits to use

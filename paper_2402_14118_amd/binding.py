@@ -24,12 +24,18 @@ MMM_ERR_INVALID_ARG, MMM_ERR_SHAPE, MMM_ERR_DTYPE, MMM_ERR_WORKSPACE, MMM_ERR_MA
 MMM_F32, MMM_BF16, MMM_F16, MMM_F64 = 0, 1, 2, 3
 MMM_PRED_NONZERO, MMM_PRED_GT, MMM_PRED_ABS_GT = 0, 1, 2
 MMM_PATH_AUTO, MMM_PATH_MATRIX, MMM_PATH_PAIRS = -1, 0, 1
+MMM_ACT_NONE, MMM_ACT_RELU, MMM_ACT_GELU, MMM_ACT_GELU_TANH, MMM_ACT_SILU = range(5)
+MMM_NORM_NONE, MMM_NORM_RMS, MMM_NORM_LAYER = range(3)
+MMM_GATE_NONE, MMM_GATE_ROW, MMM_GATE_COL, MMM_GATE_FULL = range(4)
+MMM_NORM_MAX_WIDTH = 32768
 
 EXPORTS = [
     "mmm_maps_workspace_bytes", "mmm_maps_workspace_bytes_for", "mmm_maps_init", "mmm_maps_release", "mmm_build_maps", "mmm_maps_view",
     "mmm_maps_view_derived", "mmm_maps_view_compacted", "mmm_maps_view_lists", "mmm_debug_k_lists", "mmm_maps_stats", "mmm_matmul", "mmm_matmul_static_scratch", "mmm_matmul_fused",
     "mmm_maps_set_path", "mmm_matmul_path", "mmm_matmul_form", "mmm_set_option", "mmm_matmul_variant_count",
     "mmm_matmul_variant_name", "mmm_matmul_plan", "mmm_maps_set_plan", "mmm_status_string", "mmm_last_device_error",
+    "mmm_epilogue_backward_workspace_bytes", "mmm_epilogue_backward", "mmm_block_norm",
+    "mmm_block_norm_backward_workspace_bytes", "mmm_block_norm_backward",
 ]
 
 
@@ -39,6 +45,20 @@ class MaskA(ctypes.Structure):
 
 class MaskB(ctypes.Structure):
     _fields_ = [("block_width", ctypes.c_int32), ("keep_rows", ctypes.c_void_p), ("keep_blocks", ctypes.c_void_p)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("dt", ctypes.c_int32), ("dt_h", ctypes.c_int32), ("dt_y", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate", ctypes.c_int32), ("eps", ctypes.c_float), ("alpha", ctypes.c_float)]
+
+
+class BlockNormGrads(ctypes.Structure):
+    _fields_ = [("h_out", ctypes.c_void_p), ("ldh_out", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+                ("gate_values", ctypes.c_void_p), ("ldgate", ctypes.c_int64), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("d_n", ctypes.c_void_p), ("ldd_n", ctypes.c_int64), ("d_h_out", ctypes.c_void_p),
+                ("ldd_h_out", ctypes.c_int64), ("d_h", ctypes.c_void_p), ("ldd_h", ctypes.c_int64), ("d_y", ctypes.c_void_p),
+                ("ldd_y", ctypes.c_int64), ("d_gate", ctypes.c_void_p), ("ldd_gate", ctypes.c_int64), ("d_post_weight", ctypes.c_void_p),
+                ("d_post_bias", ctypes.c_void_p), ("d_pre_weight", ctypes.c_void_p), ("d_pre_bias", ctypes.c_void_p)]
 
 
 class MmmError(RuntimeError):
@@ -82,6 +102,11 @@ def _load() -> ctypes.CDLL:
     lib.mmm_matmul_variant_name.argtypes = [i32]
     lib.mmm_matmul_variant_name.restype = c.c_char_p
     lib.mmm_matmul_plan.argtypes = [vp, i32, c.POINTER(i32), c.POINTER(i32), c.POINTER(i64)]
+    lib.mmm_epilogue_backward_workspace_bytes.argtypes = [i64, i64, c.POINTER(c.c_size_t)]
+    lib.mmm_epilogue_backward.argtypes = [i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, c.c_size_t, vp]
+    lib.mmm_block_norm.argtypes = [c.POINTER(BlockNormDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.mmm_block_norm_backward_workspace_bytes.argtypes = [i64, i64, c.POINTER(c.c_size_t)]
+    lib.mmm_block_norm_backward.argtypes = [c.POINTER(BlockNormDesc), c.POINTER(BlockNormGrads), vp, c.c_size_t, vp]
     lib.mmm_status_string.argtypes = [i32]
     lib.mmm_status_string.restype = c.c_char_p
     lib.mmm_last_device_error.restype = c.c_char_p
@@ -267,3 +292,32 @@ def mmm_matmul_plan(maps: int, dt: int):
     v, s, w = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int64(0)
     _check(lib.mmm_matmul_plan(maps, dt, ctypes.byref(v), ctypes.byref(s), ctypes.byref(w)), "mmm_matmul_plan")
     return v.value, s.value, w.value
+
+
+def mmm_epilogue_backward_workspace_bytes(M: int, N: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib.mmm_epilogue_backward_workspace_bytes(M, N, ctypes.byref(out)), "mmm_epilogue_backward_workspace_bytes")
+    return out.value
+
+
+def mmm_epilogue_backward(M: int, N: int, dt: int, out_dtype: int, activation: int, dC, lddc: int, Z, ldz: int, dZ, lddz: int, dbias=None,
+                          workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib.mmm_epilogue_backward(M, N, dt, out_dtype, activation, _ptr(dC), lddc, _ptr(Z), ldz, _ptr(dZ), lddz, _ptr(dbias), _ptr(workspace),
+                                     workspace_bytes, _stream(stream)), "mmm_epilogue_backward")
+
+
+def mmm_block_norm(desc: BlockNormDesc, h, ldh: int, y, ldy: int, gate, ldgate: int, post_weight, post_bias, pre_weight, pre_bias, h_out,
+                   ldh_out: int, n, ldn: int, stream=None) -> None:
+    _check(lib.mmm_block_norm(ctypes.byref(desc), _ptr(h), ldh, _ptr(y), ldy, _ptr(gate), ldgate, _ptr(post_weight), _ptr(post_bias),
+                              _ptr(pre_weight), _ptr(pre_bias), _ptr(h_out), ldh_out, _ptr(n), ldn, _stream(stream)), "mmm_block_norm")
+
+
+def mmm_block_norm_backward_workspace_bytes(M: int, N: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib.mmm_block_norm_backward_workspace_bytes(M, N, ctypes.byref(out)), "mmm_block_norm_backward_workspace_bytes")
+    return out.value
+
+
+def mmm_block_norm_backward(desc: BlockNormDesc, grads: BlockNormGrads, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib.mmm_block_norm_backward(ctypes.byref(desc), ctypes.byref(grads), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "mmm_block_norm_backward")

@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 
 #include "mmm_internal.h"
@@ -892,6 +893,131 @@ mmm_status mmm_matmul_static_scratch(const mmm_maps *maps, mmm_dtype dt, const v
                                      int64_t ldy, void *C, int64_t ldc, int32_t accumulate, void *hip_stream)
 {
     return matmul_common(maps, dt, X, ldx, Y, ldy, C, ldc, accumulate, hip_stream, true);
+}
+
+namespace {
+
+// types a 16-bit operator may hold its sums in: its own, or floats
+bool or_float(int32_t t, int32_t dt) { return t == dt || t == MMM_F32; }
+bool trains(int32_t dt) { return dtype_ok((mmm_dtype)dt) && dt != MMM_F64; }
+// address of elements of this type (or none)
+bool placed(const void *p, int32_t dt) { return reinterpret_cast<uintptr_t>(p) % elem_size((mmm_dtype)dt) == 0; }
+bool workspace_ok(const void *p, size_t bytes, size_t need) { return p != nullptr && reinterpret_cast<uintptr_t>(p) % kAlign == 0 && bytes >= need; }
+
+mmm_status norm_desc_ok(const mmm_block_norm_desc *d)
+{
+    if (d == nullptr) return MMM_ERR_INVALID_ARG;
+    if (!trains(d->dt) || !or_float(d->dt_h, d->dt) || !or_float(d->dt_y, d->dt)) return MMM_ERR_DTYPE;
+    if (d->post < MMM_NORM_NONE || d->post > MMM_NORM_LAYER || d->pre < MMM_NORM_NONE || d->pre > MMM_NORM_LAYER) return MMM_ERR_INVALID_ARG;
+    if (d->gate < MMM_GATE_NONE || d->gate > MMM_GATE_FULL || !(d->eps >= 0.f)) return MMM_ERR_INVALID_ARG;
+    if (d->M < 1 || d->M > (1LL << 30) || d->N < 1 || d->N > MMM_NORM_MAX_WIDTH) return MMM_ERR_SHAPE;
+    return MMM_OK;
+}
+
+// what both directions ask of the operands: (value, leading dimension, type) of those that are M x N, a row each of the others
+struct Plane { const void *p; int64_t ld; int32_t dt; };
+mmm_status planes_ok(std::initializer_list<Plane> planes, int64_t N)
+{
+    for (const Plane &q : planes)
+        if (q.p != nullptr && q.ld < N) return MMM_ERR_SHAPE;
+    for (const Plane &q : planes)
+        if (!placed(q.p, q.dt)) return MMM_ERR_DTYPE;
+    return MMM_OK;
+}
+
+}   // namespace
+
+mmm_status mmm_epilogue_backward_workspace_bytes(int64_t M, int64_t N, size_t *bytes)
+{
+    if (bytes == nullptr) return MMM_ERR_INVALID_ARG;
+    if (M < 1 || N < 1 || M > (1LL << 30) || N > (1LL << 30)) return MMM_ERR_SHAPE;
+    *bytes = align_up(mmm_epilogue_grad_bytes(M, N));
+    return MMM_OK;
+}
+
+mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype out_dtype, int32_t activation, const void *dC, int64_t lddc,
+                                 const void *Z, int64_t ldz, void *dZ, int64_t lddz, float *dbias, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream)
+{
+    if (activation < MMM_ACT_NONE || activation > MMM_ACT_SILU) return MMM_ERR_INVALID_ARG;
+    if (dC == nullptr || (Z == nullptr && activation != MMM_ACT_NONE) || (dZ == nullptr && dbias == nullptr)) return MMM_ERR_INVALID_ARG;
+    if (!trains(dt) || !or_float(out_dtype, dt)) return MMM_ERR_DTYPE;
+    size_t need = 0;
+    if (mmm_status st = mmm_epilogue_backward_workspace_bytes(M, N, &need); st != MMM_OK) return st;
+    if (mmm_status st = planes_ok({{dC, lddc, out_dtype}, {activation != MMM_ACT_NONE ? Z : nullptr, ldz, out_dtype}, {dZ, lddz, dt}, {dbias, N, MMM_F32}}, N); st != MMM_OK)
+        return st;
+    if (dbias != nullptr && !workspace_ok(workspace, workspace_bytes, need)) return MMM_ERR_WORKSPACE;
+    if (hipError_t e = mmm_launch_epilogue_grad(M, N, dt, out_dtype, activation, dC, lddc, Z, ldz, dZ, lddz, dbias, workspace, static_cast<hipStream_t>(hip_stream));
+        e != hipSuccess) {
+        note_device_error("epilogue gradient launch", e);
+        return MMM_ERR_DEVICE;
+    }
+    return MMM_OK;
+}
+
+mmm_status mmm_block_norm(const mmm_block_norm_desc *desc, const void *h, int64_t ldh, const void *y, int64_t ldy, const void *gate_values,
+                          int64_t ldgate, const void *post_weight, const void *post_bias, const void *pre_weight, const void *pre_bias,
+                          void *h_out, int64_t ldh_out, void *n, int64_t ldn, void *hip_stream)
+{
+    if (mmm_status st = norm_desc_ok(desc); st != MMM_OK) return st;
+    const mmm_block_norm_desc &d = *desc;
+    if (h == nullptr || (h_out == nullptr && n == nullptr) || (n != nullptr) != (d.pre != MMM_NORM_NONE)) return MMM_ERR_INVALID_ARG;
+    if (y == nullptr && (h_out != nullptr || d.post != MMM_NORM_NONE || d.gate != MMM_GATE_NONE)) return MMM_ERR_INVALID_ARG;
+    if ((gate_values != nullptr) != (d.gate != MMM_GATE_NONE)) return MMM_ERR_INVALID_ARG;
+    if ((d.post == MMM_NORM_NONE && (post_weight != nullptr || post_bias != nullptr)) || (d.pre == MMM_NORM_NONE && (pre_weight != nullptr || pre_bias != nullptr)))
+        return MMM_ERR_INVALID_ARG;
+    if (mmm_status st = planes_ok({{h, ldh, d.dt_h}, {y, ldy, d.dt_y}, {gate_values, d.gate == MMM_GATE_FULL ? ldgate : d.N, d.dt}, {post_weight, d.N, d.dt},
+                                   {post_bias, d.N, d.dt}, {pre_weight, d.N, d.dt}, {pre_bias, d.N, d.dt}, {h_out, ldh_out, d.dt_h}, {n, ldn, d.dt}}, d.N);
+        st != MMM_OK)
+        return st;
+    if (h_out == h && ldh_out != ldh) return MMM_ERR_SHAPE;
+    if (hipError_t e = mmm_launch_block_norm(d, h, ldh, y, ldy, gate_values, ldgate, post_weight, post_bias, pre_weight, pre_bias, h_out, ldh_out, n, ldn,
+                                             static_cast<hipStream_t>(hip_stream));
+        e != hipSuccess) {
+        note_device_error("norm launch", e);
+        return MMM_ERR_DEVICE;
+    }
+    return MMM_OK;
+}
+
+mmm_status mmm_block_norm_backward_workspace_bytes(int64_t M, int64_t N, size_t *bytes)
+{
+    if (bytes == nullptr) return MMM_ERR_INVALID_ARG;
+    if (M < 1 || M > (1LL << 30) || N < 1 || N > MMM_NORM_MAX_WIDTH) return MMM_ERR_SHAPE;
+    *bytes = align_up(mmm_block_norm_grad_bytes(M, N));
+    return MMM_OK;
+}
+
+mmm_status mmm_block_norm_backward(const mmm_block_norm_desc *desc, const mmm_block_norm_grads *grads, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream)
+{
+    if (mmm_status st = norm_desc_ok(desc); st != MMM_OK) return st;
+    if (grads == nullptr) return MMM_ERR_INVALID_ARG;
+    const mmm_block_norm_desc &d = *desc;
+    const mmm_block_norm_grads &g = *grads;
+    const bool pre = d.pre != MMM_NORM_NONE, post = d.post != MMM_NORM_NONE;
+    if ((g.d_n != nullptr) != pre || (pre && g.h_out == nullptr) || (!pre && g.d_h_out == nullptr)) return MMM_ERR_INVALID_ARG;
+    if (g.y == nullptr && (post || d.gate != MMM_GATE_NONE || g.d_y != nullptr)) return MMM_ERR_INVALID_ARG;
+    if ((g.gate_values != nullptr) != (d.gate != MMM_GATE_NONE) || (g.d_gate != nullptr && d.gate == MMM_GATE_NONE)) return MMM_ERR_INVALID_ARG;
+    if (!post && (g.post_weight != nullptr || g.post_bias != nullptr || g.d_post_weight != nullptr || g.d_post_bias != nullptr)) return MMM_ERR_INVALID_ARG;
+    if (!pre && (g.pre_weight != nullptr || g.d_pre_weight != nullptr || g.d_pre_bias != nullptr)) return MMM_ERR_INVALID_ARG;
+    const bool sums = g.d_post_weight != nullptr || g.d_post_bias != nullptr || g.d_pre_weight != nullptr || g.d_pre_bias != nullptr ||
+                      (d.gate == MMM_GATE_COL && g.d_gate != nullptr);
+    if (g.d_h == nullptr && g.d_y == nullptr && g.d_gate == nullptr && !sums) return MMM_ERR_INVALID_ARG;
+    if (mmm_status st = planes_ok({{pre ? g.h_out : nullptr, g.ldh_out, d.dt_h}, {g.y, g.ldy, d.dt_y}, {g.gate_values, d.gate == MMM_GATE_FULL ? g.ldgate : d.N, d.dt},
+                                   {g.post_weight, d.N, d.dt}, {g.post_bias, d.N, d.dt}, {g.pre_weight, d.N, d.dt}, {g.d_n, g.ldd_n, d.dt},
+                                   {g.d_h_out, g.ldd_h_out, d.dt_h}, {g.d_h, g.ldd_h, d.dt_h}, {g.d_y, g.ldd_y, d.dt_y},
+                                   {g.d_gate, d.gate == MMM_GATE_FULL ? g.ldd_gate : d.N, d.gate == MMM_GATE_FULL ? d.dt : MMM_F32},
+                                   {g.d_post_weight, d.N, MMM_F32}, {g.d_post_bias, d.N, MMM_F32}, {g.d_pre_weight, d.N, MMM_F32}, {g.d_pre_bias, d.N, MMM_F32}}, d.N);
+        st != MMM_OK)
+        return st;
+    if (g.d_h != nullptr && g.d_h == g.d_h_out && g.ldd_h != g.ldd_h_out) return MMM_ERR_SHAPE;
+    if (sums && !workspace_ok(workspace, workspace_bytes, mmm_block_norm_grad_bytes(d.M, d.N))) return MMM_ERR_WORKSPACE;
+    if (hipError_t e = mmm_launch_block_norm_grad(d, g, workspace, static_cast<hipStream_t>(hip_stream)); e != hipSuccess) {
+        note_device_error("norm gradient launch", e);
+        return MMM_ERR_DEVICE;
+    }
+    return MMM_OK;
 }
 
 mmm_status mmm_maps_set_plan(mmm_maps *maps, int32_t variant, int32_t split_k)

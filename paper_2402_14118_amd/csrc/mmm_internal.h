@@ -323,3 +323,20 @@ bool mmm_pairs_supports(int32_t dtype, int64_t ldy);
 hipError_t mmm_launch_dump_lists(const mmm_maps *m, uint8_t *out, size_t out_bytes, size_t *need, hipStream_t s);
 // device address of the library's own scratch array on the current device (MMM_STATIC_SCRATCH_BYTES bytes)
 hipError_t mmm_static_scratch(float **ptr);
+
+// ---- the operators around the product
+// what is done with the elements of the product before they are written (device form of mmm_epilogue)
+struct mmm_epilogue_args {
+    const void *bias, *residual;
+    void *preact;
+    int64_t ldr, ldp;
+    int32_t activation, out_dtype;
+};
+hipError_t mmm_launch_block_norm(const mmm_block_norm_desc &d, const void *h, int64_t ldh, const void *y, int64_t ldy, const void *gate, int64_t ldgate,
+                                 const void *post_weight, const void *post_bias, const void *pre_weight, const void *pre_bias, void *h_out,
+                                 int64_t ldh_out, void *n, int64_t ldn, hipStream_t s);
+size_t mmm_block_norm_grad_bytes(int64_t M, int64_t N);
+hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_block_norm_grads &g, void *workspace, hipStream_t s);
+size_t mmm_epilogue_grad_bytes(int64_t M, int64_t N);
+hipError_t mmm_launch_epilogue_grad(int64_t M, int64_t N, int32_t dt, int32_t out_dtype, int32_t activation, const void *dC, int64_t lddc, const void *Z,
+                                    int64_t ldz, void *dZ, int64_t lddz, float *dbias, void *workspace, hipStream_t s);

@@ -1,0 +1,105 @@
+"""What the operators around the product refuse, on the host, before any device call."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2402_14118_amd as mm
+from paper_2402_14118_amd import binding as B
+
+AT = 0x7000_0000_0000          # never dereferenced on the host
+
+
+def at(i):
+    return AT + (i << 32)
+
+
+def norm(desc, h=at(0), ldh=64, y=None, ldy=0, gate=None, ldgate=0, pw=None, pb=None, w=None, b=None, h_out=None, ldho=0, n=at(1), ldn=64):
+    return B.lib.mmm_block_norm(None if desc is None else ctypes.byref(desc), h, ldh, y, ldy, gate, ldgate, pw, pb, w, b, h_out, ldho, n, ldn, None)
+
+
+def desc(M=4, N=64, dt=0, dt_h=0, dt_y=0, post=0, pre=1, gate=0, eps=1e-5, alpha=1.0):
+    return mm.BlockNormDesc(M, N, dt, dt_h, dt_y, post, pre, gate, eps, alpha)
+
+
+def test_norm_refuses():
+    assert norm(None) == B.MMM_ERR_INVALID_ARG
+    for bad in (dict(dt=3), dict(dt=9), dict(dt_h=1), dict(dt_y=2), dict(dt=1, dt_h=2), dict(dt=1, dt_h=3)):
+        assert norm(desc(**bad)) == B.MMM_ERR_DTYPE, bad
+    for bad in (dict(M=0), dict(N=0), dict(N=mm.MMM_NORM_MAX_WIDTH + 1), dict(M=(1 << 30) + 1)):
+        assert norm(desc(**bad), ldh=1 << 20, ldn=1 << 20) == B.MMM_ERR_SHAPE, bad
+    for bad in (dict(post=3), dict(pre=-1), dict(gate=4), dict(eps=-1.0), dict(eps=float("nan"))):
+        assert norm(desc(**bad)) == B.MMM_ERR_INVALID_ARG, bad
+    d, both = desc(), desc(post=1, gate=2)
+    assert norm(d, h=None) == norm(d, n=None) == norm(desc(pre=0)) == B.MMM_ERR_INVALID_ARG
+    # no block: nothing behind it
+    assert norm(d, h_out=at(2), ldho=64) == norm(desc(post=1)) == norm(desc(gate=1), gate=at(2)) == B.MMM_ERR_INVALID_ARG
+    assert norm(d, pw=at(2)) == norm(desc(pre=0), y=at(2), ldy=64, h_out=at(3), ldho=64, n=None, w=at(4)) == B.MMM_ERR_INVALID_ARG
+    # the gate that is announced, and no other
+    assert norm(both, y=at(2), ldy=64) == norm(desc(post=1), y=at(2), ldy=64, gate=at(3)) == B.MMM_ERR_INVALID_ARG
+    assert norm(d, ldh=63) == norm(d, ldn=63) == norm(both, y=at(2), ldy=63, gate=at(3)) == B.MMM_ERR_SHAPE
+    assert norm(desc(post=1, gate=3), y=at(2), ldy=64, gate=at(3), ldgate=63) == B.MMM_ERR_SHAPE
+    assert norm(both, y=at(2), ldy=64, gate=at(3), h_out=at(0), ldho=65) == B.MMM_ERR_SHAPE      # in place is in place
+    assert norm(d, h=at(0) + 2) == norm(d, w=at(2) + 1) == norm(both, y=at(2), ldy=64, gate=at(3) + 2) == B.MMM_ERR_DTYPE
+
+
+def grads(d, ws=at(20), nbytes=1 << 30, **k):
+    g = mm.BlockNormGrads()
+    for name, v in k.items():
+        setattr(g, name, v)
+    return B.lib.mmm_block_norm_backward(ctypes.byref(d), ctypes.byref(g), ws, nbytes, None)
+
+
+def test_norm_backward_refuses():
+    full = dict(h_out=at(0), ldh_out=64, y=at(1), ldy=64, gate_values=at(2), d_n=at(3), ldd_n=64, d_h=at(4), ldd_h=64, d_pre_weight=at(5))
+    d = desc(post=1, gate=2)
+    assert B.lib.mmm_block_norm_backward(ctypes.byref(d), None, None, 0, None) == B.MMM_ERR_INVALID_ARG
+    # with what is asked for nothing missing, a workspace that is too small is what is left to refuse
+    assert grads(d, nbytes=16, **full) == B.MMM_ERR_WORKSPACE
+    assert grads(d, ws=None, **full) == grads(d, ws=at(20) + 8, **full) == B.MMM_ERR_WORKSPACE
+    assert grads(d, nbytes=mm.mmm_block_norm_backward_workspace_bytes(4, 64) - 256, **full) == B.MMM_ERR_WORKSPACE
+
+    def without(*names, **more):
+        return grads(d, nbytes=16, **{k: v for k, v in full.items() if k not in names}, **more)
+    for missing in ("h_out", "y", "gate_values", "d_n"):
+        assert without(missing) == B.MMM_ERR_INVALID_ARG, missing
+    assert without("d_h", "d_pre_weight") == B.MMM_ERR_INVALID_ARG        # nothing asked for
+    assert without("ldh_out") == without("ldd_n") == without("ldd_h") == without("ldy") == B.MMM_ERR_SHAPE
+    assert without(d_h_out=at(4), ldd_h_out=65) == B.MMM_ERR_SHAPE
+    assert without("d_pre_weight", d_pre_weight=at(5) + 2) == B.MMM_ERR_DTYPE
+    # no norm in front: its operands are not taken, and a gradient has to come in
+    p = desc(post=1, pre=0)
+    assert grads(p, y=at(1), ldy=64, d_y=at(4), ldd_y=64) == B.MMM_ERR_INVALID_ARG
+    assert grads(p, y=at(1), ldy=64, d_y=at(4), ldd_y=64, d_h_out=at(5), ldd_h_out=64, d_pre_bias=at(6)) == B.MMM_ERR_INVALID_ARG
+    n = ctypes.c_size_t(0)
+    assert B.lib.mmm_block_norm_backward_workspace_bytes(0, 8, ctypes.byref(n)) == B.MMM_ERR_SHAPE
+    assert B.lib.mmm_block_norm_backward_workspace_bytes(8, 40000, ctypes.byref(n)) == B.MMM_ERR_SHAPE
+    assert B.lib.mmm_block_norm_backward_workspace_bytes(8, 8, None) == B.MMM_ERR_INVALID_ARG
+
+
+def test_epilogue_backward_refuses():
+    def call(M=4, N=16, dt=1, out=1, act=1, dC=at(0), lddc=16, Z=at(1), ldz=16, dZ=at(2), lddz=16, db=None, ws=None, n=0):
+        return B.lib.mmm_epilogue_backward(M, N, dt, out, act, dC, lddc, Z, ldz, dZ, lddz, db, ws, n, None)
+    assert call(act=5) == call(act=-1) == call(dC=None) == call(Z=None) == call(dZ=None) == B.MMM_ERR_INVALID_ARG
+    assert call(dt=3, out=3) == call(dt=1, out=2) == call(dt=0, out=1) == call(dt=4) == B.MMM_ERR_DTYPE
+    assert call(M=0) == call(N=0) == call(lddc=15) == call(ldz=15) == call(lddz=15) == B.MMM_ERR_SHAPE
+    assert call(dC=at(0) + 1) == call(Z=at(1) + 1) == call(dZ=at(2) + 1) == call(db=at(3) + 2, ws=at(4), n=1 << 20) == B.MMM_ERR_DTYPE
+    need = mm.mmm_epilogue_backward_workspace_bytes(4, 16)
+    assert call(db=at(3)) == call(db=at(3), ws=at(4), n=need - 1) == call(db=at(3), ws=at(4) + 128, n=need) == B.MMM_ERR_WORKSPACE
+    n = ctypes.c_size_t(0)
+    assert B.lib.mmm_epilogue_backward_workspace_bytes(0, 1, ctypes.byref(n)) == B.MMM_ERR_SHAPE
+    assert B.lib.mmm_epilogue_backward_workspace_bytes(1, 1, None) == B.MMM_ERR_INVALID_ARG
+
+
+def test_the_holder_checks_tensors(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    norm = mm.BlockNorm(4, 16, mm.MMM_BF16, post=mm.MMM_NORM_RMS, gate=mm.MMM_GATE_ROW, device="cpu")
+    H = torch.zeros(4, 16, dtype=torch.bfloat16)
+    for bad, error in ((dict(H=H[:3]), ValueError), (dict(H=H.float()), TypeError), (dict(H=H.t().contiguous().t()), ValueError), (dict(H=None), ValueError),
+                       (dict(Y=H[:, :8]), ValueError), (dict(gate=torch.zeros(16, dtype=torch.bfloat16)), ValueError), (dict(pre_weight=torch.zeros(16)), TypeError)):
+        with pytest.raises(error):
+            norm.forward(**{"H": H, "normed": torch.empty_like(H), **bad})
+    with pytest.raises(mm.MmmError):
+        mm.BlockNorm(0, 16, device="cpu")
+    with pytest.raises(ValueError):
+        mm.BlockNorm(4, 16, mm.MMM_BF16, device="cpu").forward(H, normed=torch.empty_like(H), gate=H[0])
