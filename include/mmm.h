@@ -340,8 +340,15 @@ mmm_status mmm_matmul_static_scratch(const mmm_maps *maps, mmm_dtype dt,
                                      const void *X, int64_t ldx, const void *Y, int64_t ldy,
                                      void *C, int64_t ldc, int32_t accumulate, void *hip_stream);
 
-/* ---- The operators around the product, and their gradients.  Conventions as above.  Everything is computed in float and rounded to
- * nearest even once, where it is written to a 16-bit type. */
+/* ---- The operators around the product: those of a residual block whose second product is a masked one.
+ *
+ *     n  = norm(h)                                  mmm_block_norm
+ *     a  = act(M(n) x N(W1) + b1)                   mmm_matmul_epilogue   (its zeros are the sparsity of the next product)
+ *     y  = M(a) x N(W2) + b2                        mmm_matmul_epilogue
+ *     h' = alpha h + gate norm(y), n' = norm(h')    mmm_block_norm        (n' is what the next block starts from)
+ *
+ * and their gradients: mmm_epilogue_backward, mmm_block_norm_backward.  Conventions as above.  Everything is
+ * computed in float (double for double inputs) and rounded to nearest even once, where it is written to a 16-bit type. */
 
 typedef enum {
     MMM_ACT_NONE = 0,
@@ -350,6 +357,30 @@ typedef enum {
     MMM_ACT_GELU_TANH = 3,   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2              */
     MMM_ACT_SILU = 4         /* z / (1 + exp(-z))                                              */
 } mmm_activation;
+
+/* What is done with an element of the product before it is written:
+ *     Z[i,j] = sum[i,j] + bias[j]        C[i,j] = act(Z[i,j]) + residual[i,j] */
+typedef struct {
+    int32_t activation;     /* mmm_activation                                                                  */
+    int32_t out_dtype;      /* mmm_dtype of C, residual and preact: the type of the inputs, or MMM_F32 for 16-bit inputs */
+    const void *bias;       /* optional, N elements of the type of the inputs                                  */
+    const void *residual;   /* optional, M x ldr, out_dtype; may be C itself with ldr == ldc (C is then added to) */
+    int64_t ldr;
+    void *preact;           /* optional, M x ldp, out_dtype: Z, which the gradient of the activation is taken at; overlaps nothing else */
+    int64_t ldp;
+} mmm_epilogue;
+
+/* C = act(A x B + bias) + residual.  With ma == NULL the product is that of mmm_matmul, and everything said there about X, Y and the
+ * maps holds; with ma it is that of mmm_matmul_fused (the mask evaluated inside the multiplication; only the B side of the maps is
+ * used; meant for few rows).  The sums are those of these calls: kernel, plan and order are the same, so that C rounded to
+ * float is theirs bit by bit where nothing is done in the epilogue.  Rows of A and columns of B without any product give act(bias) + residual.
+ * The activation and all that follows are computed in the type of the sums, whatever out_dtype is.
+ * Partial sums of a split K lie in the workspace of the maps, as mmm_matmul's: two calls on one handle that may run at the same time race.
+ * Errors: MMM_ERR_INVALID_ARG (NULL pointer, unknown activation, bad mask), MMM_ERR_SHAPE (a leading dimension too small),
+ * MMM_ERR_DTYPE (out_dtype not allowed, misaligned pointer), MMM_ERR_MAPS_MISMATCH, MMM_ERR_DEVICE. */
+mmm_status mmm_matmul_epilogue(const mmm_maps *maps, mmm_dtype dt,
+                               const void *X, int64_t ldx, const mmm_mask_a *ma, const void *Y, int64_t ldy,
+                               void *C, int64_t ldc, const mmm_epilogue *epilogue, void *hip_stream);
 
 /* The gradient through the epilogue:
  *     dZ[i,j] = dC[i,j] act'(Z[i,j])        dbias[j] = sum over i of dC[i,j] act'(Z[i,j])

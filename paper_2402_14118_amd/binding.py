@@ -34,7 +34,7 @@ EXPORTS = [
     "mmm_maps_view_derived", "mmm_maps_view_compacted", "mmm_maps_view_lists", "mmm_debug_k_lists", "mmm_maps_stats", "mmm_matmul", "mmm_matmul_static_scratch", "mmm_matmul_fused",
     "mmm_maps_set_path", "mmm_matmul_path", "mmm_matmul_form", "mmm_set_option", "mmm_matmul_variant_count",
     "mmm_matmul_variant_name", "mmm_matmul_plan", "mmm_maps_set_plan", "mmm_status_string", "mmm_last_device_error",
-    "mmm_epilogue_backward_workspace_bytes", "mmm_epilogue_backward", "mmm_block_norm",
+    "mmm_matmul_epilogue", "mmm_epilogue_backward_workspace_bytes", "mmm_epilogue_backward", "mmm_block_norm",
     "mmm_block_norm_backward_workspace_bytes", "mmm_block_norm_backward",
 ]
 
@@ -45,6 +45,11 @@ class MaskA(ctypes.Structure):
 
 class MaskB(ctypes.Structure):
     _fields_ = [("block_width", ctypes.c_int32), ("keep_rows", ctypes.c_void_p), ("keep_blocks", ctypes.c_void_p)]
+
+
+class Epilogue(ctypes.Structure):
+    _fields_ = [("activation", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("ldr", ctypes.c_int64), ("preact", ctypes.c_void_p), ("ldp", ctypes.c_int64)]
 
 
 class BlockNormDesc(ctypes.Structure):
@@ -102,6 +107,7 @@ def _load() -> ctypes.CDLL:
     lib.mmm_matmul_variant_name.argtypes = [i32]
     lib.mmm_matmul_variant_name.restype = c.c_char_p
     lib.mmm_matmul_plan.argtypes = [vp, i32, c.POINTER(i32), c.POINTER(i32), c.POINTER(i64)]
+    lib.mmm_matmul_epilogue.argtypes = [vp, i32, vp, i64, c.POINTER(MaskA), vp, i64, vp, i64, c.POINTER(Epilogue), vp]
     lib.mmm_epilogue_backward_workspace_bytes.argtypes = [i64, i64, c.POINTER(c.c_size_t)]
     lib.mmm_epilogue_backward.argtypes = [i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, c.c_size_t, vp]
     lib.mmm_block_norm.argtypes = [c.POINTER(BlockNormDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp]
@@ -144,6 +150,10 @@ def _ptr(t) -> Optional[int]:
 # The current stream's handle straight from torch's runtime: building a Stream object takes 2.8 us a call.
 _get_device = getattr(torch._C, "_cuda_getDevice", None)
 _get_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def current_device() -> int:
+    return _get_device() if _get_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
 def _stream(stream) -> Optional[int]:
@@ -292,6 +302,13 @@ def mmm_matmul_plan(maps: int, dt: int):
     v, s, w = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int64(0)
     _check(lib.mmm_matmul_plan(maps, dt, ctypes.byref(v), ctypes.byref(s), ctypes.byref(w)), "mmm_matmul_plan")
     return v.value, s.value, w.value
+
+
+def mmm_matmul_epilogue(maps: int, dt: int, X, ldx: int, ma: Optional[MaskA], Y, ldy: int, C, ldc: int, epilogue: Epilogue, stream=None) -> None:
+    e = epilogue
+    _check(native.matmul_epilogue(maps, dt, _ptr(X), ldx, ma is not None, *((ma.pred, ma.threshold, ma.keep_bits) if ma is not None else _NO_MASK),
+                                  _ptr(Y), ldy, _ptr(C), ldc, e.activation, e.out_dtype, e.bias, e.residual, e.ldr, e.preact, e.ldp,
+                                  _stream(stream)), "mmm_matmul_epilogue")
 
 
 def mmm_epilogue_backward_workspace_bytes(M: int, N: int) -> int:

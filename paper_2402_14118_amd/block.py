@@ -10,38 +10,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
-
-TORCH_TYPES = {B.MMM_F32: torch.float32, B.MMM_BF16: torch.bfloat16, B.MMM_F16: torch.float16, B.MMM_F64: torch.float64}
-
-
-def _rows(name: str, t: Optional[torch.Tensor], shape, dtype: int, device, optional: bool = True):
-    """(tensor, leading dimension) of a matrix, or of a vector (leading dimension 0), as the C ABI takes it."""
-    if t is None:
-        if not optional:
-            raise ValueError(f"{name} is needed")
-        return None, 0
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if t.dtype != TORCH_TYPES[dtype]:
-        raise TypeError(f"{name} is {t.dtype}, not {TORCH_TYPES[dtype]}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"the elements of {name} are not neighbours in memory")
-    if t.dim() == 1:
-        return t, 0
-    return t, (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
-
-
-def _own_device(device) -> torch.device:
-    d = torch.device(device)
-    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
-
-
-def _check_device(device: torch.device) -> None:
-    """Kernels are launched on the current device, and on its current stream where none is given."""
-    if device.type == "cuda" and torch.cuda.current_device() != device.index:
-        raise ValueError(f"the current device is cuda:{torch.cuda.current_device()}, the tensors are on {device}")
+from .tensors import check_device, own_device, rows
 
 
 class BlockNorm:
@@ -58,7 +27,7 @@ class BlockNorm:
                  alpha: float = 1.0, eps: float = 1e-5, dtype_h: Optional[int] = None, dtype_y: Optional[int] = None, training: bool = False,
                  device="cuda:0"):
         self.desc = B.BlockNormDesc(M, N, dtype, dtype if dtype_h is None else dtype_h, dtype if dtype_y is None else dtype_y, post, pre, gate, eps, alpha)
-        self.device = _own_device(device)
+        self.device = own_device(device)
         nbytes = B.mmm_block_norm_backward_workspace_bytes(M, N)   # (checks M and N)
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if training else None
 
@@ -67,21 +36,21 @@ class BlockNorm:
         shape = {B.MMM_GATE_ROW: (d.M,), B.MMM_GATE_COL: (d.N,), B.MMM_GATE_FULL: (d.M, d.N)}.get(d.gate)
         if shape is None and t is not None:
             raise ValueError(f"{name} is given, but there is no gate")
-        return _rows(name, t, shape, B.MMM_F32 if sums and d.gate != B.MMM_GATE_FULL else d.dt, self.device)
+        return rows(name, t, shape, B.MMM_F32 if sums and d.gate != B.MMM_GATE_FULL else d.dt, self.device)
 
     def _vector(self, name, t, dtype):
-        return _rows(name, t, (self.desc.N,), dtype, self.device)[0]
+        return rows(name, t, (self.desc.N,), dtype, self.device)[0]
 
     def forward(self, H: torch.Tensor, normed: Optional[torch.Tensor] = None, H_out: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
                 gate: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
                 pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
         """H_out may be H."""
         d, shape = self.desc, (self.desc.M, self.desc.N)
-        _check_device(self.device)
-        B.mmm_block_norm(d, *_rows("H", H, shape, d.dt_h, self.device, False), *_rows("Y", Y, shape, d.dt_y, self.device), *self._gate("gate", gate),
+        check_device(self.device)
+        B.mmm_block_norm(d, *rows("H", H, shape, d.dt_h, self.device, False), *rows("Y", Y, shape, d.dt_y, self.device), *self._gate("gate", gate),
                          self._vector("post_weight", post_weight, d.dt), self._vector("post_bias", post_bias, d.dt),
                          self._vector("pre_weight", pre_weight, d.dt), self._vector("pre_bias", pre_bias, d.dt),
-                         *_rows("H_out", H_out, shape, d.dt_h, self.device), *_rows("normed", normed, shape, d.dt, self.device), stream)
+                         *rows("H_out", H_out, shape, d.dt_h, self.device), *rows("normed", normed, shape, d.dt, self.device), stream)
 
     def backward(self, H_out: Optional[torch.Tensor] = None, grad_normed: Optional[torch.Tensor] = None, grad_H_out: Optional[torch.Tensor] = None,
                  grad_H: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
@@ -93,14 +62,14 @@ class BlockNorm:
         not worked out; those of weights, biases and of a gate per row or column are float."""
         d, shape, f = self.desc, (self.desc.M, self.desc.N), B.MMM_F32
         p = B._ptr
-        _check_device(self.device)
-        ho, ldho = _rows("H_out", H_out, shape, d.dt_h, self.device)
-        y, ldy = _rows("Y", Y, shape, d.dt_y, self.device)
+        check_device(self.device)
+        ho, ldho = rows("H_out", H_out, shape, d.dt_h, self.device)
+        y, ldy = rows("Y", Y, shape, d.dt_y, self.device)
         ga, ldga = self._gate("gate", gate)
-        dn, lddn = _rows("grad_normed", grad_normed, shape, d.dt, self.device)
-        dho, lddho = _rows("grad_H_out", grad_H_out, shape, d.dt_h, self.device)
-        dh, lddh = _rows("grad_H", grad_H, shape, d.dt_h, self.device)
-        dy, lddy = _rows("grad_Y", grad_Y, shape, d.dt_y, self.device)
+        dn, lddn = rows("grad_normed", grad_normed, shape, d.dt, self.device)
+        dho, lddho = rows("grad_H_out", grad_H_out, shape, d.dt_h, self.device)
+        dh, lddh = rows("grad_H", grad_H, shape, d.dt_h, self.device)
+        dy, lddy = rows("grad_Y", grad_Y, shape, d.dt_y, self.device)
         dg, lddg = self._gate("grad_gate", grad_gate, sums=True)
         g = B.BlockNormGrads(p(ho), ldho, p(y), ldy, p(ga), ldga, p(self._vector("post_weight", post_weight, d.dt)),
                              p(self._vector("post_bias", post_bias, d.dt)), p(self._vector("pre_weight", pre_weight, d.dt)), p(dn), lddn, p(dho), lddho,

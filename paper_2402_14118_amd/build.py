@@ -12,8 +12,9 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmmm_hip.so")
 NATIVE = os.path.join(PKG, "_mmm_native.so")       # CPython entry points, linked against the library
 NATIVE_SOURCE = os.path.join(CSRC, "mmm_python.cpp")
-SOURCES = ["mmm_api.hip", "mmm_build.hip", "mmm_matmul.hip", "mmm_pairs.hip", "mmm_norm.hip"]
-HEADERS = [os.path.join(CSRC, "mmm_internal.h"), os.path.join(CSRC, "mmm_elements.h"), os.path.join(ROOT, "include", "mmm.h")]
+SOURCES = ["mmm_api.hip", "mmm_build.hip", "mmm_matmul.hip", "mmm_matmul_epilogue.hip", "mmm_pairs.hip", "mmm_norm.hip"]
+HEADERS = [os.path.join(CSRC, "mmm_internal.h"), os.path.join(CSRC, "mmm_elements.h"), os.path.join(CSRC, "mmm_matmul_kernel.h"),
+            os.path.join(ROOT, "include", "mmm.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")

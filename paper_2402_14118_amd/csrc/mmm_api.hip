@@ -797,8 +797,23 @@ mmm_status mmm_matmul_plan(const mmm_maps *maps, mmm_dtype dt, int32_t *variant,
 
 }   // extern "C"
 
-static mmm_status matmul_common(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y, int64_t ldy,
-                                void *C, int64_t ldc, int32_t accumulate, void *hip_stream, bool static_scratch)
+// the epilogue as kernels take it; MMM_OK where there is none
+static mmm_status epilogue_of(const mmm_maps *maps, mmm_dtype dt, const mmm_epilogue *e, mmm_epilogue_args *args)
+{
+    if (e == nullptr) return MMM_OK;
+    if (e->activation < MMM_ACT_NONE || e->activation > MMM_ACT_SILU) return MMM_ERR_INVALID_ARG;
+    if (e->out_dtype != dt && (e->out_dtype != MMM_F32 || dt == MMM_F64)) return MMM_ERR_DTYPE;
+    if ((e->residual != nullptr && e->ldr < maps->N) || (e->preact != nullptr && e->ldp < maps->N)) return MMM_ERR_SHAPE;
+    const size_t esz = elem_size(e->out_dtype);
+    if (reinterpret_cast<uintptr_t>(e->bias) % elem_size(dt) != 0 || reinterpret_cast<uintptr_t>(e->residual) % esz != 0 ||
+        reinterpret_cast<uintptr_t>(e->preact) % esz != 0)
+        return MMM_ERR_DTYPE;
+    *args = {e->bias, e->residual, e->preact, e->ldr, e->ldp, e->activation, e->out_dtype};
+    return MMM_OK;
+}
+
+static mmm_status matmul_common(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y, int64_t ldy, void *C, int64_t ldc,
+                                int32_t accumulate, void *hip_stream, bool static_scratch, const mmm_epilogue *epilogue = nullptr)
 {
     if (maps == nullptr || X == nullptr || Y == nullptr || C == nullptr) return MMM_ERR_INVALID_ARG;
     if (!dtype_ok(dt)) return MMM_ERR_DTYPE;
@@ -806,8 +821,10 @@ static mmm_status matmul_common(const mmm_maps *maps, mmm_dtype dt, const void *
     if (ldx > kMaxLd || ldy > kMaxLd) return MMM_ERR_SHAPE;   // tile-relative offsets are 32-bit
     const size_t esz = elem_size(dt);
     if (reinterpret_cast<uintptr_t>(X) % esz != 0 || reinterpret_cast<uintptr_t>(Y) % esz != 0 ||
-        reinterpret_cast<uintptr_t>(C) % c_elem_size(dt) != 0)
+        reinterpret_cast<uintptr_t>(C) % (epilogue != nullptr ? elem_size(epilogue->out_dtype) : c_elem_size(dt)) != 0)
         return MMM_ERR_DTYPE;
+    mmm_epilogue_args epi{};
+    if (mmm_status st = epilogue_of(maps, dt, epilogue, &epi); st != MMM_OK) return st;
     if (dt == MMM_F64 && !mmm_pairs_supports(dt, ldy)) return MMM_ERR_SHAPE;   // for every double Y, whichever kernel it is
     if (!maps->a_built || !maps->b_built) return MMM_ERR_MAPS_MISMATCH;
     if (maps->a_dtype != dt || maps->b_dtype != dt) return MMM_ERR_MAPS_MISMATCH;
@@ -820,8 +837,9 @@ static mmm_status matmul_common(const mmm_maps *maps, mmm_dtype dt, const void *
     if (pairs_can && (!packed_y || choose_path(maps, dt, maps->b_form) == MMM_PATH_PAIRS)) {   // no scratch at all on this path
         hipError_t e = ensure_bt(maps, static_cast<hipStream_t>(hip_stream));
         if (e == hipSuccess)
-            e = mmm_launch_pairs(maps, dt, X, ldx, Y, ldy, C, ldc, accumulate ? 1 : 0, false, 0, 0.f, nullptr,
-                                 static_cast<hipStream_t>(hip_stream));
+            e = epilogue != nullptr ? mmm_launch_pairs_epilogue(maps, dt, X, ldx, Y, ldy, C, ldc, epi, false, 0, 0.f, nullptr, static_cast<hipStream_t>(hip_stream))
+                                    : mmm_launch_pairs(maps, dt, X, ldx, Y, ldy, C, ldc, accumulate ? 1 : 0, false, 0, 0.f, nullptr,
+                                                       static_cast<hipStream_t>(hip_stream));
         if (e != hipSuccess) {
             note_device_error("masked GEMM (pairs) launch", e);
             return MMM_ERR_DEVICE;
@@ -846,10 +864,41 @@ static mmm_status matmul_common(const mmm_maps *maps, mmm_dtype dt, const void *
         }
         partial_bytes = (size_t)MMM_STATIC_SCRATCH_BYTES;
     }
-    if (hipError_t e = mmm_launch_matmul(maps, p, dt, C, ldc, accumulate ? 1 : 0, partials, partial_bytes,
-                                         static_cast<hipStream_t>(hip_stream));
+    if (hipError_t e = epilogue != nullptr
+                           ? mmm_launch_matmul_epilogue(maps, p, dt, C, ldc, epi, partials, partial_bytes, static_cast<hipStream_t>(hip_stream))
+                           : mmm_launch_matmul(maps, p, dt, C, ldc, accumulate ? 1 : 0, partials, partial_bytes, static_cast<hipStream_t>(hip_stream));
         e != hipSuccess) {
         note_device_error("masked GEMM launch", e);
+        return MMM_ERR_DEVICE;
+    }
+    return MMM_OK;
+}
+
+static mmm_status fused_common(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const mmm_mask_a *ma, const void *Y, int64_t ldy, void *C,
+                               int64_t ldc, int32_t accumulate, void *hip_stream, const mmm_epilogue *epilogue = nullptr)
+{
+    if (maps == nullptr || X == nullptr || Y == nullptr || C == nullptr || ma == nullptr) return MMM_ERR_INVALID_ARG;
+    if (ma->pred < MMM_PRED_NONZERO || ma->pred > MMM_PRED_ABS_GT) return MMM_ERR_INVALID_ARG;
+    if (ma->keep_bits != nullptr && reinterpret_cast<uintptr_t>(ma->keep_bits) % 8 != 0) return MMM_ERR_INVALID_ARG;
+    if (!dtype_ok(dt)) return MMM_ERR_DTYPE;
+    if (ldx < maps->K || ldy < maps->N || ldc < maps->N) return MMM_ERR_SHAPE;
+    if (ldx > kMaxLd || ldy > kMaxLd) return MMM_ERR_SHAPE;
+    const size_t esz = elem_size(dt);
+    if (reinterpret_cast<uintptr_t>(X) % esz != 0 || reinterpret_cast<uintptr_t>(Y) % esz != 0 ||
+        reinterpret_cast<uintptr_t>(C) % (epilogue != nullptr ? elem_size(epilogue->out_dtype) : c_elem_size(dt)) != 0)
+        return MMM_ERR_DTYPE;
+    mmm_epilogue_args epi{};
+    if (mmm_status st = epilogue_of(maps, dt, epilogue, &epi); st != MMM_OK) return st;
+    if (!mmm_pairs_supports(dt, ldy)) return MMM_ERR_SHAPE;
+    if (!maps->b_built || maps->b_dtype != dt) return MMM_ERR_MAPS_MISMATCH;
+    hipError_t e = ensure_bt(maps, static_cast<hipStream_t>(hip_stream));
+    if (e == hipSuccess)
+        e = epilogue != nullptr ? mmm_launch_pairs_epilogue(maps, dt, X, ldx, Y, ldy, C, ldc, epi, true, ma->pred, ma->threshold, ma->keep_bits,
+                                                            static_cast<hipStream_t>(hip_stream))
+                                : mmm_launch_pairs(maps, dt, X, ldx, Y, ldy, C, ldc, accumulate ? 1 : 0, true, ma->pred, ma->threshold, ma->keep_bits,
+                                                   static_cast<hipStream_t>(hip_stream));
+    if (e != hipSuccess) {
+        note_device_error("fused masked GEMM launch", e);
         return MMM_ERR_DEVICE;
     }
     return MMM_OK;
@@ -866,27 +915,16 @@ mmm_status mmm_matmul(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t
 mmm_status mmm_matmul_fused(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const mmm_mask_a *ma,
                             const void *Y, int64_t ldy, void *C, int64_t ldc, int32_t accumulate, void *hip_stream)
 {
-    if (maps == nullptr || X == nullptr || Y == nullptr || C == nullptr || ma == nullptr) return MMM_ERR_INVALID_ARG;
-    if (ma->pred < MMM_PRED_NONZERO || ma->pred > MMM_PRED_ABS_GT) return MMM_ERR_INVALID_ARG;
-    if (ma->keep_bits != nullptr && reinterpret_cast<uintptr_t>(ma->keep_bits) % 8 != 0) return MMM_ERR_INVALID_ARG;
-    if (!dtype_ok(dt)) return MMM_ERR_DTYPE;
-    if (ldx < maps->K || ldy < maps->N || ldc < maps->N) return MMM_ERR_SHAPE;
-    if (ldx > kMaxLd || ldy > kMaxLd) return MMM_ERR_SHAPE;
-    const size_t esz = elem_size(dt);
-    if (reinterpret_cast<uintptr_t>(X) % esz != 0 || reinterpret_cast<uintptr_t>(Y) % esz != 0 ||
-        reinterpret_cast<uintptr_t>(C) % c_elem_size(dt) != 0)
-        return MMM_ERR_DTYPE;
-    if (!mmm_pairs_supports(dt, ldy)) return MMM_ERR_SHAPE;
-    if (!maps->b_built || maps->b_dtype != dt) return MMM_ERR_MAPS_MISMATCH;
-    hipError_t e = ensure_bt(maps, static_cast<hipStream_t>(hip_stream));
-    if (e == hipSuccess)
-        e = mmm_launch_pairs(maps, dt, X, ldx, Y, ldy, C, ldc, accumulate ? 1 : 0, true, ma->pred, ma->threshold, ma->keep_bits,
-                             static_cast<hipStream_t>(hip_stream));
-    if (e != hipSuccess) {
-        note_device_error("fused masked GEMM launch", e);
-        return MMM_ERR_DEVICE;
-    }
-    return MMM_OK;
+    return fused_common(maps, dt, X, ldx, ma, Y, ldy, C, ldc, accumulate, hip_stream);
+}
+
+mmm_status mmm_matmul_epilogue(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const mmm_mask_a *ma, const void *Y, int64_t ldy,
+                               void *C, int64_t ldc, const mmm_epilogue *epilogue, void *hip_stream)
+{
+    if (epilogue == nullptr) return MMM_ERR_INVALID_ARG;
+    if (C != nullptr && epilogue->residual == C && epilogue->ldr != ldc) return MMM_ERR_SHAPE;
+    if (ma != nullptr) return fused_common(maps, dt, X, ldx, ma, Y, ldy, C, ldc, 0, hip_stream, epilogue);
+    return matmul_common(maps, dt, X, ldx, Y, ldy, C, ldc, 0, hip_stream, false, epilogue);
 }
 
 mmm_status mmm_matmul_static_scratch(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y,

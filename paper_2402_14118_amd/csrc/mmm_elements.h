@@ -4,7 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "mmm.h"
+#include "mmm_internal.h"
 
 // what a type is computed in
 template <typename T> struct mmm_wide { typedef float type; };
@@ -57,24 +57,24 @@ template <typename E> __device__ __forceinline__ E mmm_sigmoid(E v) { return E(1
 
 // act(z).  GELU is z times the normal distribution function, written with erfc, which keeps its digits for negative z; its tanh
 // form is z times a sigmoid: (1 + tanh u) / 2 = sigmoid(2 u).  An infinite -z is 0 in the limit, where z times 0 is NaN.
-template <typename E> __device__ __forceinline__ E mmm_activated(E z, int32_t act)
+template <typename E, int N> __device__ __forceinline__ void mmm_activate(E (&z)[N], int32_t act)
 {
-    switch (act) {
-    case MMM_ACT_RELU: return z < E(0) ? E(0) : z;
-    case MMM_ACT_GELU: {
-        const E p = E(0.5) * mmm_erfc(z * E(-0.70710678118654752440));
-        return p == E(0) ? E(0) : z * p;
+    if (act == MMM_ACT_RELU) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) z[q] = z[q] < E(0) ? E(0) : z[q];
+    } else if (act != MMM_ACT_NONE) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            E p;
+            if (act == MMM_ACT_GELU)
+                p = E(0.5) * mmm_erfc(z[q] * E(-0.70710678118654752440));
+            else if (act == MMM_ACT_GELU_TANH)
+                p = mmm_sigmoid(E(1.5957691216057307117) * z[q] * (E(1) + E(0.044715) * z[q] * z[q]));   // 2 sqrt(2 / pi)
+            else
+                p = mmm_sigmoid(z[q]);
+            z[q] = p == E(0) ? E(0) : z[q] * p;
+        }
     }
-    case MMM_ACT_GELU_TANH: {
-        const E p = mmm_sigmoid(E(1.5957691216057307117) * z * (E(1) + E(0.044715) * z * z));   // 2 sqrt(2 / pi)
-        return p == E(0) ? E(0) : z * p;
-    }
-    case MMM_ACT_SILU: {
-        const E p = mmm_sigmoid(z);
-        return p == E(0) ? E(0) : z * p;
-    }
-    }
-    return z;
 }
 
 // act'(z); that of ReLU at 0 is 0.  The terms with z vanish in both limits.
@@ -98,3 +98,57 @@ __device__ __forceinline__ float mmm_slope(float z, int32_t act)
     }
     return 1.f;
 }
+
+// N neighbours of a row of either type, as E
+template <typename T, typename E, int N> __device__ __forceinline__ void mmm_load_as(const void *base, int64_t at, E (&out)[N])
+{
+    typedef typename mmm_row_piece<T, N>::type piece;
+    const piece v = *reinterpret_cast<const piece *>(static_cast<const T *>(base) + at);
+#pragma unroll
+    for (int q = 0; q < N; ++q) out[q] = (E)v[q];
+}
+template <typename T, typename E, int N> __device__ __forceinline__ void mmm_store_as(void *base, int64_t at, const E (&in)[N])
+{
+    typedef typename mmm_row_piece<T, N>::type piece;
+    piece v;
+#pragma unroll
+    for (int q = 0; q < N; ++q) v[q] = (T)in[q];
+    *reinterpret_cast<piece *>(static_cast<T *>(base) + at) = v;
+}
+
+// The epilogue of N neighbours of rows of C: what is the same in every row, and what is done to one.  T: type of the inputs, E: of the sums.
+template <typename T, typename E, int N> struct mmm_column_values {
+    E bias[N];
+    __device__ __forceinline__ void load(const mmm_epilogue_args &e, int64_t col)
+    {
+#pragma unroll
+        for (int q = 0; q < N; ++q) bias[q] = E(0);
+        if (e.bias != nullptr) mmm_load_as<T, E, N>(e.bias, col, bias);
+    }
+    __device__ __forceinline__ void finish(const mmm_epilogue_args &e, const E (&sum)[N], void *C, int64_t ldc, int64_t row, int64_t col) const
+    {
+        const bool wide = sizeof(T) == sizeof(E) || e.out_dtype == MMM_F32;
+        auto load = [&](const void *base, int64_t ld, E (&out)[N]) __attribute__((always_inline)) {
+            if (wide)
+                mmm_load_as<E, E, N>(base, row * ld + col, out);
+            else
+                mmm_load_as<T, E, N>(base, row * ld + col, out);
+        };
+        auto store = [&](void *base, int64_t ld, const E (&in)[N]) __attribute__((always_inline)) {
+            if (wide)
+                mmm_store_as<E, E, N>(base, row * ld + col, in);
+            else
+                mmm_store_as<T, E, N>(base, row * ld + col, in);
+        };
+        E z[N], more[N];
+        if (e.residual != nullptr) load(e.residual, e.ldr, more);
+#pragma unroll
+        for (int q = 0; q < N; ++q) z[q] = e.bias != nullptr ? sum[q] + bias[q] : sum[q];
+        if (e.preact != nullptr) store(e.preact, e.ldp, z);
+        mmm_activate(z, e.activation);
+        if (e.residual != nullptr)
+#pragma unroll
+            for (int q = 0; q < N; ++q) z[q] += more[q];
+        store(C, ldc, z);
+    }
+};

@@ -332,6 +332,12 @@ struct mmm_epilogue_args {
     int64_t ldr, ldp;
     int32_t activation, out_dtype;
 };
+hipError_t mmm_launch_tiles(const mmm_maps *m, const mmm_plan &p, int32_t dtype, void *C, int64_t ldc, int32_t accumulate, void *partials,
+                            size_t partial_bytes, hipStream_t s);   // mmm_launch_matmul without the sum over the parts of K
+hipError_t mmm_launch_matmul_epilogue(const mmm_maps *m, const mmm_plan &p, int32_t dtype, void *C, int64_t ldc, const mmm_epilogue_args &epilogue,
+                                      void *partials, size_t partial_bytes, hipStream_t s);
+hipError_t mmm_launch_pairs_epilogue(const mmm_maps *m, int32_t dtype, const void *X, int64_t ldx, const void *Y, int64_t ldy, void *C, int64_t ldc,
+                                     const mmm_epilogue_args &epilogue, bool fused, int32_t pred, float threshold, const uint64_t *keep_a, hipStream_t s);
 hipError_t mmm_launch_block_norm(const mmm_block_norm_desc &d, const void *h, int64_t ldh, const void *y, int64_t ldy, const void *gate, int64_t ldgate,
                                  const void *post_weight, const void *post_bias, const void *pre_weight, const void *pre_bias, void *h_out,
                                  int64_t ldh_out, void *n, int64_t ldn, hipStream_t s);

@@ -33,6 +33,7 @@
 // pass is needed.
 #include <type_traits>
 
+#include "mmm_elements.h"
 #include "mmm_internal.h"
 
 namespace {
@@ -58,6 +59,9 @@ struct PairsParams {
     uint32_t workgroups;
 };
 
+struct PairsEpilogueParams : PairsParams { mmm_epilogue_args epilogue; };
+template <bool EPI> using ParamsOf = std::conditional_t<EPI, PairsEpilogueParams, PairsParams>;
+
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef double doublex2 __attribute__((ext_vector_type(2)));
@@ -71,11 +75,12 @@ template <> struct Row16<8> { typedef u32x4 type __attribute__((aligned(8), may_
 __device__ __forceinline__ float fma_acc(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
 __device__ __forceinline__ double fma_acc(double a, double b, double c) { return __builtin_fma(a, b, c); }
 
-// Per element type: the type products are accumulated in (float; double for double inputs), the exact widening of an
+// Per element type: the type products are accumulated in (float; double for double inputs), the type as the epilogue takes it, the exact widening of an
 // element to it, and of the elements of 16 bytes; the bit pattern the predicate is decided on (as in the map builder).
 template <typename T> struct Elem;
 template <> struct Elem<float> {
     typedef float acc;
+    typedef float model;
     typedef uint32_t pattern;
     static __device__ __forceinline__ acc value(float v) { return v; }
     static __device__ __forceinline__ void unpack(u32x4 v, acc *out)
@@ -86,6 +91,7 @@ template <> struct Elem<float> {
 };
 template <> struct Elem<uint16_t> {   // bf16
     typedef float acc;
+    typedef __bf16 model;
     typedef uint32_t pattern;
     static __device__ __forceinline__ acc value(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ void unpack(u32x4 v, acc *out)
@@ -99,6 +105,7 @@ template <> struct Elem<uint16_t> {   // bf16
 };
 template <> struct Elem<_Float16> {
     typedef float acc;
+    typedef _Float16 model;
     typedef uint32_t pattern;
     static __device__ __forceinline__ acc value(_Float16 v) { return (float)v; }
     static __device__ __forceinline__ void unpack(u32x4 v, acc *out)
@@ -111,6 +118,7 @@ template <> struct Elem<_Float16> {
 };
 template <> struct Elem<double> {
     typedef double acc;
+    typedef double model;
     typedef uint64_t pattern;
     static __device__ __forceinline__ acc value(double v) { return v; }
     static __device__ __forceinline__ void unpack(u32x4 v, acc *out)
@@ -130,8 +138,9 @@ __device__ __forceinline__ uint32_t pairs_xcd_id(uint32_t b, uint32_t n)
 // CW: waves side by side (64 columns each); KS: waves that share a column span and take the
 // 4096-wide ranges of k in turn (their partial sums are added in a fixed order at the end).
 // WAVE_WORDS: map words one wave intersects at a time (a range of 64 * WAVE_WORDS values of k).
-template <typename T, int BW, int CW, int KS, int WAVE_WORDS, bool FUSED>
-__global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUSED ? 4 : 8, 8))) void mmm_pairs_kernel(const PairsParams p)
+// EPI: bias, activation and residual on the way to C.
+template <typename T, int BW, int CW, int KS, int WAVE_WORDS, bool FUSED, bool EPI>
+__global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUSED ? 4 : 8, 8))) void mmm_pairs_kernel(const ParamsOf<EPI> p)
 {
     static_assert(WAVE_WORDS <= MAX_WAVE_WORDS && WAVE_WORDS % BW == 0, "whole words per lane, offsets fit the lists");
     constexpr int NW = CW * KS;
@@ -397,12 +406,19 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
             for (int q = 1; q < KS; ++q) acc[0] += red[((q - 1) * CW + cw) * 64 + lane];
     }
     if (ks == 0 && col < p.N) {
-        acc_t *dst = static_cast<acc_t *>(p.C) + (int64_t)row_i * p.ldc + col;
-        *dst = p.accumulate ? *dst + acc[0] : acc[0];
+        if constexpr (EPI) {
+            const acc_t sum[1] = {acc[0]};
+            mmm_column_values<typename Elem<T>::model, acc_t, 1> column;
+            column.load(p.epilogue, col);
+            column.finish(p.epilogue, sum, p.C, p.ldc, row_i, col);
+        } else {
+            acc_t *dst = static_cast<acc_t *>(p.C) + (int64_t)row_i * p.ldc + col;
+            *dst = p.accumulate ? *dst + acc[0] : acc[0];
+        }
     }
 }
 
-typedef void (*pairs_kernel_fn)(const PairsParams);
+template <bool EPI> using pairs_kernel_fn = void (*)(const ParamsOf<EPI>);
 
 struct PairsShape { int cw, ks, words; };
 
@@ -412,26 +428,26 @@ struct PairsShape { int cw, ks, words; };
 //   8 x 2, 4 x 4, 2 x 8  few rows, mask evaluated here: the predicate work is shared by 512, 256, 128 columns
 // Words: the fewest that still give every share a part of K (64 k each), so that no wave stands idle: a K of 4096 in ranges
 // of 64 words was one range, for one wave in four.
-template <typename T, int BW, bool FUSED> pairs_kernel_fn pick_shape(const PairsShape &sh)
+template <typename T, int BW, bool FUSED, bool EPI> pairs_kernel_fn<EPI> pick_shape(const PairsShape &sh)
 {
     constexpr int W16 = BW == 32 ? 32 : 16;   // a lane takes at least one word
     const int w = sh.words;
     if (sh.ks == 1)
-        return w == 16 ? mmm_pairs_kernel<T, BW, 8, 1, W16, FUSED> : w == 32 ? mmm_pairs_kernel<T, BW, 8, 1, 32, FUSED> : mmm_pairs_kernel<T, BW, 8, 1, 64, FUSED>;
+        return w == 16 ? mmm_pairs_kernel<T, BW, 8, 1, W16, FUSED, EPI> : w == 32 ? mmm_pairs_kernel<T, BW, 8, 1, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 8, 1, 64, FUSED, EPI>;
     if constexpr (!FUSED) {
-        return w == 16 ? mmm_pairs_kernel<T, BW, 2, 4, W16, FUSED> : w == 32 ? mmm_pairs_kernel<T, BW, 2, 4, 32, FUSED> : mmm_pairs_kernel<T, BW, 2, 4, 64, FUSED>;
+        return w == 16 ? mmm_pairs_kernel<T, BW, 2, 4, W16, FUSED, EPI> : w == 32 ? mmm_pairs_kernel<T, BW, 2, 4, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 2, 4, 64, FUSED, EPI>;
     } else {
-        if (sh.ks == 8) return w == 16 ? mmm_pairs_kernel<T, BW, 2, 8, W16, FUSED> : mmm_pairs_kernel<T, BW, 2, 8, 32, FUSED>;
-        if (sh.ks == 4) return w <= 32 ? mmm_pairs_kernel<T, BW, 4, 4, 32, FUSED> : mmm_pairs_kernel<T, BW, 4, 4, 64, FUSED>;
-        return w <= 32 ? mmm_pairs_kernel<T, BW, 8, 2, 32, FUSED> : mmm_pairs_kernel<T, BW, 8, 2, 64, FUSED>;
+        if (sh.ks == 8) return w == 16 ? mmm_pairs_kernel<T, BW, 2, 8, W16, FUSED, EPI> : mmm_pairs_kernel<T, BW, 2, 8, 32, FUSED, EPI>;
+        if (sh.ks == 4) return w <= 32 ? mmm_pairs_kernel<T, BW, 4, 4, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 4, 4, 64, FUSED, EPI>;
+        return w <= 32 ? mmm_pairs_kernel<T, BW, 8, 2, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 8, 2, 64, FUSED, EPI>;
     }
 }
 
-template <typename T, bool FUSED> pairs_kernel_fn pick(int32_t bw, const PairsShape &sh)
+template <bool EPI, typename T, bool FUSED> pairs_kernel_fn<EPI> pick(int32_t bw, const PairsShape &sh)
 {
-    if (bw == 8) return pick_shape<T, 8, FUSED>(sh);
-    if (bw == 16) return pick_shape<T, 16, FUSED>(sh);
-    return pick_shape<T, 32, FUSED>(sh);
+    if (bw == 8) return pick_shape<T, 8, FUSED, EPI>(sh);
+    if (bw == 16) return pick_shape<T, 16, FUSED, EPI>(sh);
+    return pick_shape<T, 32, FUSED, EPI>(sh);
 }
 
 }   // namespace
@@ -443,11 +459,13 @@ bool mmm_pairs_supports(int32_t dtype, int64_t ldy)
 }
 
 // fused: evaluate M (pred, threshold, keep_a) on X in the kernel; otherwise take a_bits from the maps.
-hipError_t mmm_launch_pairs(const mmm_maps *m, int32_t dtype, const void *X, int64_t ldx, const void *Y, int64_t ldy,
-                            void *C, int64_t ldc, int32_t accumulate, bool fused, int32_t pred, float threshold,
-                            const uint64_t *keep_a, hipStream_t s)
+template <bool EPI>
+static hipError_t launch_pairs(const mmm_maps *m, int32_t dtype, const void *X, int64_t ldx, const void *Y, int64_t ldy,
+                               void *C, int64_t ldc, int32_t accumulate, const mmm_epilogue_args &epilogue, bool fused, int32_t pred, float threshold,
+                               const uint64_t *keep_a, hipStream_t s)
 {
-    PairsParams p{};
+    ParamsOf<EPI> p{};
+    if constexpr (EPI) p.epilogue = epilogue;
     p.X = X;
     p.ldx = ldx;
     p.Y = Y;
@@ -489,15 +507,28 @@ hipError_t mmm_launch_pairs(const mmm_maps *m, int32_t dtype, const void *X, int
     const int64_t ctiles = (m->N + span - 1) / span;
     const int64_t wgs = ctiles * m->M;
     if (wgs <= 0 || wgs > 0x7fffffffLL) return hipErrorInvalidValue;
-    pairs_kernel_fn fn;
+    pairs_kernel_fn<EPI> fn;
     if (fused)
-        fn = dtype == MMM_F64 ? pick<double, true>(m->bw, sh) : dtype == MMM_BF16 ? pick<uint16_t, true>(m->bw, sh) : dtype == MMM_F16 ? pick<_Float16, true>(m->bw, sh)
-                                                                                         : pick<float, true>(m->bw, sh);
+        fn = dtype == MMM_F64 ? pick<EPI, double, true>(m->bw, sh) : dtype == MMM_BF16 ? pick<EPI, uint16_t, true>(m->bw, sh) : dtype == MMM_F16 ? pick<EPI, _Float16, true>(m->bw, sh)
+                                                                                         : pick<EPI, float, true>(m->bw, sh);
     else
-        fn = dtype == MMM_F64 ? pick<double, false>(m->bw, sh) : dtype == MMM_BF16 ? pick<uint16_t, false>(m->bw, sh) : dtype == MMM_F16 ? pick<_Float16, false>(m->bw, sh)
-                                                                                          : pick<float, false>(m->bw, sh);
+        fn = dtype == MMM_F64 ? pick<EPI, double, false>(m->bw, sh) : dtype == MMM_BF16 ? pick<EPI, uint16_t, false>(m->bw, sh) : dtype == MMM_F16 ? pick<EPI, _Float16, false>(m->bw, sh)
+                                                                                          : pick<EPI, float, false>(m->bw, sh);
     p.workgroups = (uint32_t)wgs;
     (void)hipGetLastError();
     hipLaunchKernelGGL(fn, dim3((uint32_t)wgs), dim3((uint32_t)(sh.cw * sh.ks * 64)), 0, s, p);
     return hipGetLastError();
+}
+
+hipError_t mmm_launch_pairs(const mmm_maps *m, int32_t dtype, const void *X, int64_t ldx, const void *Y, int64_t ldy,
+                            void *C, int64_t ldc, int32_t accumulate, bool fused, int32_t pred, float threshold,
+                            const uint64_t *keep_a, hipStream_t s)
+{
+    return launch_pairs<false>(m, dtype, X, ldx, Y, ldy, C, ldc, accumulate, {}, fused, pred, threshold, keep_a, s);
+}
+
+hipError_t mmm_launch_pairs_epilogue(const mmm_maps *m, int32_t dtype, const void *X, int64_t ldx, const void *Y, int64_t ldy, void *C, int64_t ldc,
+                                     const mmm_epilogue_args &epilogue, bool fused, int32_t pred, float threshold, const uint64_t *keep_a, hipStream_t s)
+{
+    return launch_pairs<true>(m, dtype, X, ldx, Y, ldy, C, ldc, 0, epilogue, fused, pred, threshold, keep_a, s);
 }

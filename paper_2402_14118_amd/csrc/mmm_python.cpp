@@ -1,5 +1,5 @@
-// CPython entry points for the three calls a program makes per step (mmm_build_maps, mmm_matmul,
-// mmm_matmul_fused).  They do what the ctypes functions of binding.py do -- marshal integers and call
+// CPython entry points for the calls a program makes per step (mmm_build_maps, mmm_matmul,
+// mmm_matmul_fused, mmm_matmul_epilogue).  They do what the ctypes functions of binding.py do -- marshal integers and call
 // the C ABI -- at 0.3 instead of about 3 us per call: a small problem is bound by the host, where a
 // kernel launch alone takes 3.5 us.  Pointers are passed as integers (None = NULL).  The GIL is
 // released around the call, as ctypes does.
@@ -115,10 +115,42 @@ PyObject *matmul_fused(PyObject *, PyObject *const *v, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
+// matmul_epilogue(maps, dtype, X, ldx, has_ma, pred, threshold, keep_a, Y, ldy, C, ldc, activation, out_dtype, bias, residual, ldr, preact, ldp,
+// stream)
+PyObject *matmul_epilogue(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!arity("matmul_epilogue", n, 20)) return nullptr;
+    Args a{v};
+    const mmm_maps *maps = static_cast<const mmm_maps *>(a.ptr(0));
+    const mmm_dtype dt = (mmm_dtype)a.num(1);
+    const void *X = a.ptr(2);
+    const int64_t ldx = a.num(3);
+    const bool has_ma = a.num(4) != 0;
+    const mmm_mask_a ma{(int32_t)a.num(5), a.real(6), static_cast<const uint64_t *>(a.ptr(7))};
+    const void *Y = a.ptr(8);
+    const int64_t ldy = a.num(9);
+    void *C = a.ptr(10);
+    const int64_t ldc = a.num(11);
+    const int32_t activation = (int32_t)a.num(12), out_dtype = (int32_t)a.num(13);
+    const void *bias = a.ptr(14), *residual = a.ptr(15);
+    const int64_t ldr = a.num(16);
+    void *preact = a.ptr(17);
+    const int64_t ldp = a.num(18);
+    const mmm_epilogue e{activation, out_dtype, bias, residual, ldr, preact, ldp};
+    void *stream = a.ptr(19);
+    if (!a.ok) return nullptr;
+    mmm_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = mmm_matmul_epilogue(maps, dt, X, ldx, has_ma ? &ma : nullptr, Y, ldy, C, ldc, &e, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
 PyMethodDef methods[] = {
     {"build_maps", (PyCFunction)(void (*)(void))build_maps, METH_FASTCALL, nullptr},
     {"matmul", (PyCFunction)(void (*)(void))matmul, METH_FASTCALL, nullptr},
     {"matmul_fused", (PyCFunction)(void (*)(void))matmul_fused, METH_FASTCALL, nullptr},
+    {"matmul_epilogue", (PyCFunction)(void (*)(void))matmul_epilogue, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

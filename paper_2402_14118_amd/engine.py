@@ -10,12 +10,13 @@ from typing import Optional
 import torch
 
 from . import binding as B
+from .tensors import CODES, check_device, own_device, rows
 
 
 class MaskedMatmul:
     def __init__(self, M: int, K: int, N: int, block_width: int, dtype: int = B.MMM_F32, device="cuda:0"):
         self.M, self.K, self.N, self.bw, self.dtype = M, K, N, block_width, dtype
-        self.device = torch.device(device)
+        self.device = own_device(device)
         nbytes = B.mmm_maps_workspace_bytes_for(M, K, N, block_width, dtype)
         # torch's caching allocator hands out >= 512-byte aligned blocks
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
@@ -60,6 +61,23 @@ class MaskedMatmul:
         B._check(B.native.matmul_fused(self.maps, self.dtype, X.data_ptr(), X.stride(0), pred, threshold, B._ptr(keep_a),
                                        Y.data_ptr(), Y.stride(0), C.data_ptr(), C.stride(0), int(accumulate), B._stream(stream)),
                  "mmm_matmul_fused")
+
+    def matmul_epilogue(self, X: torch.Tensor, Y: torch.Tensor, C: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                        activation: int = B.MMM_ACT_NONE, residual: Optional[torch.Tensor] = None, preact: Optional[torch.Tensor] = None,
+                        pred: Optional[int] = None, threshold: float = 0.0, keep_a: Optional[torch.Tensor] = None, stream=None) -> None:
+        """C = activation(A x B + bias) + residual; preact receives A x B + bias.  C, residual and preact are of one type: that of the
+        inputs, or float.  residual may be C.  With a predicate M is evaluated inside the multiplication, as in matmul_fused."""
+        check_device(self.device)
+        dev, dt, shape, out = self.device, self.dtype, (self.M, self.N), CODES.get(C.dtype, -1)
+        x, ldx = rows("X", X, (self.M, self.K), dt, dev, False)
+        y, ldy = rows("Y", Y, (self.K, self.N), dt, dev, False)
+        c, ldc = rows("C", C, shape, out, dev, False)
+        r, ldr = rows("residual", residual, shape, out, dev)
+        z, ldp = rows("preact", preact, shape, out, dev)
+        b = rows("bias", bias, (self.N,), dt, dev)[0]
+        B._check(B.native.matmul_epilogue(self.maps, dt, x.data_ptr(), ldx, pred is not None, 0 if pred is None else pred, threshold, B._ptr(keep_a),
+                                          y.data_ptr(), ldy, c.data_ptr(), ldc, activation, out, B._ptr(b), B._ptr(r), ldr, B._ptr(z), ldp,
+                                          B._stream(stream)), "mmm_matmul_epilogue")
 
     def set_path(self, path: int = -1) -> None:
         B.mmm_maps_set_path(self.maps, path)

@@ -1,0 +1,42 @@
+"""Tensors as the C ABI takes them: checks of shape, type, device and layout, and the leading dimension."""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+TORCH_TYPES = {B.MMM_F32: torch.float32, B.MMM_BF16: torch.bfloat16, B.MMM_F16: torch.float16, B.MMM_F64: torch.float64}
+CODES = {t: code for code, t in TORCH_TYPES.items()}
+
+
+def rows(name: str, t: Optional[torch.Tensor], shape, dtype: int, device, optional: bool = True):
+    """(tensor, leading dimension) of a matrix, or of a vector (leading dimension 0)."""
+    if t is None:
+        if not optional:
+            raise ValueError(f"{name} is needed")
+        return None, 0
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype is not TORCH_TYPES.get(dtype):
+        raise TypeError(f"{name} is {t.dtype}, not {TORCH_TYPES.get(dtype)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"the elements of {name} are not neighbours in memory")
+    if len(shape) == 1:
+        return t, 0
+    return t, (strides[0] if shape[0] > 1 else max(strides[0], shape[1]))
+
+
+def own_device(device) -> torch.device:
+    d = torch.device(device)
+    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
+def check_device(device: torch.device) -> None:
+    """Kernels are launched on the current device, and on its current stream where none is given."""
+    if device.type == "cuda" and B.current_device() != device.index:
+        raise ValueError(f"the current device is cuda:{B.current_device()}, the tensors are on {device}")

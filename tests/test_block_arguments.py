@@ -91,8 +91,7 @@ def test_epilogue_backward_refuses():
     assert B.lib.mmm_epilogue_backward_workspace_bytes(1, 1, None) == B.MMM_ERR_INVALID_ARG
 
 
-def test_the_holder_checks_tensors(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+def test_the_holder_checks_tensors():
     norm = mm.BlockNorm(4, 16, mm.MMM_BF16, post=mm.MMM_NORM_RMS, gate=mm.MMM_GATE_ROW, device="cpu")
     H = torch.zeros(4, 16, dtype=torch.bfloat16)
     for bad, error in ((dict(H=H[:3]), ValueError), (dict(H=H.float()), TypeError), (dict(H=H.t().contiguous().t()), ValueError), (dict(H=None), ValueError),
@@ -103,3 +102,44 @@ def test_the_holder_checks_tensors(monkeypatch):
         mm.BlockNorm(0, 16, device="cpu")
     with pytest.raises(ValueError):
         mm.BlockNorm(4, 16, mm.MMM_BF16, device="cpu").forward(H, normed=torch.empty_like(H), gate=H[0])
+
+
+def test_matmul_epilogue_refuses():
+    need = mm.mmm_maps_workspace_bytes(64, 128, 64, 16)
+    maps = mm.mmm_maps_init(AT, need, 64, 128, 64, 16)
+    ma = mm.MaskA(0, 0.0, None)
+
+    def call(dt=1, X=at(1), ldx=128, mask=None, Y=at(2), ldy=64, C=at(3), ldc=64, e="default", handle=maps, **k):
+        e = mm.Epilogue(**{"activation": 1, "out_dtype": dt, **k}) if e == "default" else e
+        return B.lib.mmm_matmul_epilogue(handle, dt, X, ldx, None if mask is None else ctypes.byref(mask), Y, ldy, C, ldc, None if e is None else ctypes.byref(e), None)
+    try:
+        for mask in (None, ma):
+            assert call(mask=mask) == B.MMM_ERR_MAPS_MISMATCH       # nothing is built: what is refused below is refused before that
+            assert call(mask=mask, e=None) == call(mask=mask, C=None) == call(mask=mask, handle=None) == B.MMM_ERR_INVALID_ARG
+            assert call(mask=mask, activation=5) == call(mask=mask, activation=-1) == B.MMM_ERR_INVALID_ARG
+            assert call(mask=mask, out_dtype=2) == call(mask=mask, out_dtype=3) == call(mask=mask, dt=3, out_dtype=0) == B.MMM_ERR_DTYPE
+            assert call(mask=mask, dt=0, out_dtype=1) == call(mask=mask, out_dtype=7) == B.MMM_ERR_DTYPE
+            assert call(mask=mask, out_dtype=0) == call(mask=mask, dt=3, Y=at(2)) == B.MMM_ERR_MAPS_MISMATCH
+            assert call(mask=mask, ldc=63) == call(mask=mask, residual=at(4), ldr=63) == call(mask=mask, preact=at(4), ldp=63) == B.MMM_ERR_SHAPE
+            assert call(mask=mask, residual=at(3), ldr=65) == B.MMM_ERR_SHAPE                   # in place is in place
+            assert call(mask=mask, bias=at(4) + 1) == call(mask=mask, residual=at(4) + 1, ldr=64) == call(mask=mask, preact=at(4) + 1, ldp=64) == B.MMM_ERR_DTYPE
+            assert call(mask=mask, C=at(3) + 1) == call(mask=mask, C=at(3) + 2, out_dtype=0) == B.MMM_ERR_DTYPE
+            assert call(mask=mask, C=at(3) + 2) == B.MMM_ERR_MAPS_MISMATCH                      # a 16-bit C starts at any of its elements
+        assert call(mask=mm.MaskA(3, 0.0, None)) == call(mask=mm.MaskA(0, 0.0, at(5) + 4)) == B.MMM_ERR_INVALID_ARG
+    finally:
+        mm.mmm_maps_release(maps)
+
+
+def test_the_engine_checks_tensors_of_the_epilogue():
+    eng = object.__new__(mm.MaskedMatmul)
+    eng.M, eng.K, eng.N, eng.dtype, eng.device, eng.maps = 4, 8, 16, mm.MMM_BF16, torch.device("cpu"), None
+    h = torch.bfloat16
+    X, Y, C = torch.zeros(4, 8, dtype=h), torch.zeros(8, 16, dtype=h), torch.zeros(4, 16, dtype=h)
+    for bad, error in ((dict(X=X.float()), TypeError), (dict(Y=Y[:4]), ValueError), (dict(bias=C[0].float()), TypeError),
+                       (dict(bias=C[0, :8]), ValueError), (dict(residual=C.float()), TypeError), (dict(preact=C[:2]), ValueError),
+                       (dict(C=torch.zeros(16, 4, dtype=h).t()), ValueError)):
+        with pytest.raises(error):
+            eng.matmul_epilogue(**{"X": X, "Y": Y, "C": C, **bad}, stream=0)
+    with pytest.raises(mm.MmmError) as e:
+        eng.matmul_epilogue(X, Y, C, stream=0)
+    assert e.value.status == B.MMM_ERR_INVALID_ARG
