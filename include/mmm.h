@@ -347,7 +347,7 @@ mmm_status mmm_matmul_static_scratch(const mmm_maps *maps, mmm_dtype dt,
  *     y  = M(a) x N(W2) + b2                        mmm_matmul_epilogue
  *     h' = alpha h + gate norm(y), n' = norm(h')    mmm_block_norm        (n' is what the next block starts from)
  *
- * and their gradients: mmm_epilogue_backward, mmm_block_norm_backward.  Conventions as above.  Everything is
+ * and their gradients: mmm_matmul_backward, mmm_epilogue_backward, mmm_block_norm_backward.  Conventions as above.  Everything is
  * computed in float (double for double inputs) and rounded to nearest even once, where it is written to a 16-bit type. */
 
 typedef enum {
@@ -394,6 +394,21 @@ mmm_status mmm_epilogue_backward_workspace_bytes(int64_t M, int64_t N, size_t *b
 mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype out_dtype, int32_t activation,
                                  const void *dC, int64_t lddc, const void *Z, int64_t ldz, void *dZ, int64_t lddz,
                                  float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The gradients of the product A x B under the maps as built (which are held fixed):
+ *     dX[i,k] = a_bits[i,k] ? sum over j with b_bits[k, j div bw] of dC[i,j] Y[k,j] : 0
+ *     dY[k,j] = b_bits[k, j div bw] ? sum over i with a_bits[i,k] of X[i,k] dC[i,j] : 0
+ * A zero element of X and a block of Y that holds only zeros thus get none.  X, Y, dC (M x lddc) and dX have type dt; dY is float. dX or dY may
+ * be NULL (not both).  accumulate != 0: dY += instead (unoccupied blocks stay as they are).  dX and dY overlap no input.
+ * X must be the one the A side was built from (address, ldx); the Y given is what is read, under the maps as built.
+ * Masked-out elements of X and unoccupied blocks of Y never reach the arithmetic, whatever they hold.  Elements of dC are expected
+ * to be finite: one that is not makes row i of dX and column j of dY non-finite, or less than that.
+ * Sums in float, in an order that depends on the shape and the maps only.  Nothing of the workspace is written.
+ * Errors: MMM_ERR_INVALID_ARG, MMM_ERR_SHAPE (also: a leading dimension of 2^22 and more), MMM_ERR_DTYPE (doubles; misaligned pointer), MMM_ERR_MAPS_MISMATCH (as
+ * mmm_matmul), MMM_ERR_DEVICE. */
+mmm_status mmm_matmul_backward(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y, int64_t ldy,
+                               const void *dC, int64_t lddc, void *dX, int64_t lddx, float *dY, int64_t lddy,
+                               int32_t accumulate, void *hip_stream);
 
 /* The norms around a block.  For every row i of N elements:
  *     v  = norm_post(y) * post_weight + post_bias          (post == MMM_NORM_NONE: v = y)

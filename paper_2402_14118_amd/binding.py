@@ -34,7 +34,7 @@ EXPORTS = [
     "mmm_maps_view_derived", "mmm_maps_view_compacted", "mmm_maps_view_lists", "mmm_debug_k_lists", "mmm_maps_stats", "mmm_matmul", "mmm_matmul_static_scratch", "mmm_matmul_fused",
     "mmm_maps_set_path", "mmm_matmul_path", "mmm_matmul_form", "mmm_set_option", "mmm_matmul_variant_count",
     "mmm_matmul_variant_name", "mmm_matmul_plan", "mmm_maps_set_plan", "mmm_status_string", "mmm_last_device_error",
-    "mmm_matmul_epilogue", "mmm_epilogue_backward_workspace_bytes", "mmm_epilogue_backward", "mmm_block_norm",
+    "mmm_matmul_epilogue", "mmm_matmul_backward", "mmm_epilogue_backward_workspace_bytes", "mmm_epilogue_backward", "mmm_block_norm",
     "mmm_block_norm_backward_workspace_bytes", "mmm_block_norm_backward",
 ]
 
@@ -108,6 +108,7 @@ def _load() -> ctypes.CDLL:
     lib.mmm_matmul_variant_name.restype = c.c_char_p
     lib.mmm_matmul_plan.argtypes = [vp, i32, c.POINTER(i32), c.POINTER(i32), c.POINTER(i64)]
     lib.mmm_matmul_epilogue.argtypes = [vp, i32, vp, i64, c.POINTER(MaskA), vp, i64, vp, i64, c.POINTER(Epilogue), vp]
+    lib.mmm_matmul_backward.argtypes = [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp]
     lib.mmm_epilogue_backward_workspace_bytes.argtypes = [i64, i64, c.POINTER(c.c_size_t)]
     lib.mmm_epilogue_backward.argtypes = [i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, c.c_size_t, vp]
     lib.mmm_block_norm.argtypes = [c.POINTER(BlockNormDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp]
@@ -309,6 +310,12 @@ def mmm_matmul_epilogue(maps: int, dt: int, X, ldx: int, ma: Optional[MaskA], Y,
     _check(native.matmul_epilogue(maps, dt, _ptr(X), ldx, ma is not None, *((ma.pred, ma.threshold, ma.keep_bits) if ma is not None else _NO_MASK),
                                   _ptr(Y), ldy, _ptr(C), ldc, e.activation, e.out_dtype, e.bias, e.residual, e.ldr, e.preact, e.ldp,
                                   _stream(stream)), "mmm_matmul_epilogue")
+
+
+def mmm_matmul_backward(maps: int, dt: int, X, ldx: int, Y, ldy: int, dC, lddc: int, dX, lddx: int, dY, lddy: int, accumulate: int = 0,
+                        stream=None) -> None:
+    _check(lib.mmm_matmul_backward(maps, dt, _ptr(X), ldx, _ptr(Y), ldy, _ptr(dC), lddc, _ptr(dX), lddx, _ptr(dY), lddy, int(accumulate),
+                                   _stream(stream)), "mmm_matmul_backward")
 
 
 def mmm_epilogue_backward_workspace_bytes(M: int, N: int) -> int:

@@ -1,0 +1,398 @@
+// Gradients of the masked product under the maps as built (mmm_matmul_backward):
+//     dX[i,k] = a_bits[i,k] ? sum over j of dC[i,j] B[k,j] : 0         B = N(Y), A = M(X)
+//     dY[k,j] = b_bits[k,jb] ? sum over i of A[i,k] dC[i,j] : 0
+// Both on matrix instructions, over all k, or in row-compacted mode over the live rows k' alone, whose number and places the maps hold.
+// Zeros of A inside a tile and blocks of B that are off are multiplied as zeros (their elements are not random here: A's zeros decide which of the
+// results are wanted, 64 x 128 of which share a tile); what is not wanted is dropped at the end.
+//
+// One kernel for both: a workgroup owns a tile of `TR` x `TL` results and walks the contraction in steps of 128 bytes (64 elements of the 16-bit types, 32
+// floats).  R is the operand along which a lane holds four neighbouring results, so that they are stored together; L the other.
+//               R                          L
+//     dX        rows of Y, k               rows of dC, i              contraction j, contiguous in both
+//     dY        columns of dC, j           columns of A, k            contraction i
+// A comes from the image that the builder made, masked, compacted and with 16 (floats: 4) rows of a column side by side, which is the
+// order that an operand of dY wants.  dC is read row by row there, and turned by ds_read_b64_tr_b16 (floats: one by one) on the way out of LDS.
+// Operands wait in registers while the step before is multiplied, and are laid into the other half of LDS behind it: masks are applied on the
+// way, one barrier per step.  In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that
+// eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
+#include <algorithm>
+#include <type_traits>
+
+#include "mmm_internal.h"
+
+namespace {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// 16 bytes of a row, which starts at any element
+template <int ESZ> struct AnyPiece { typedef u32x4 type __attribute__((aligned(2), may_alias)); };
+template <> struct AnyPiece<4> { typedef u32x4 type __attribute__((aligned(4), may_alias)); };
+
+constexpr int ROWB = 128;   // bytes of the contraction per step
+
+struct GradParams {
+    const void *Y, *dC;
+    int64_t ldy, lddc;
+    void *out;           // dX, of T, or dY, float
+    int64_t ldo;
+    const char *a_img;
+    const uint64_t *a_bits, *b_bits;
+    const uint32_t *kinfo, *kmap;   // row-compacted mode; else null
+    int64_t M, K, N, WA, WB;
+    int32_t KBA, steps, bw_shift, accumulate;
+    bool parts;          // the image is of floats in parts
+};
+
+template <typename T> __device__ __forceinline__ void multiply(const u32x4 &r, const u32x4 &l, floatx4 &acc)
+{
+    if constexpr (std::is_same_v<T, float>) {
+        const floatx4 a = __builtin_bit_cast(floatx4, r), b = __builtin_bit_cast(floatx4, l);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u], b[u], acc, 0, 0, 0);
+    } else if constexpr (std::is_same_v<T, _Float16>) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, r), __builtin_bit_cast(halfx8, l), acc, 0, 0, 0);
+    } else {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), __builtin_bit_cast(bf16x8, l), acc, 0, 0, 0);
+    }
+}
+
+// T: float, _Float16 or __bf16.  WR x WL waves, each FR x FL tiles of 16 x 16.
+template <typename T, bool TO_X, int WR, int WL, int FR, int FL>
+__global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradParams p)
+{
+    constexpr int ESZ = (int)sizeof(T), NT = 64 * WR * WL, TR = 16 * FR * WR, TL = 16 * FL * WL;
+    constexpr int STEP = ROWB / ESZ, PER = 16 / ESZ;          // elements of the contraction per step, and of a piece
+    constexpr int NL = TL * 8 / NT, NR = TR * 8 / NT;         // pieces of 16 bytes per thread and step
+    constexpr int TURNED_ROW = TR * ESZ, PIECES = TR / PER;   // dY: a row of dC in LDS, bytes and pieces
+    constexpr uint32_t OUTSIDE = 0x80000000u;                 // past the end of the buffers below, whatever else is added
+    static_assert(NL * NT == TL * 8 && NR * NT == TR * 8, "whole pieces");
+    __shared__ __align__(16) char lds[2][(TL + TR) * ROWB];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, s = lane >> 4, wr = wave % WR, wl = wave / WR;
+    // Tiles there are: in row-compacted mode the live ones, which the device knows.  Dealt out so that an XCD's workgroups share rows of both operands in its
+    // L2: a contiguous range of tiles, in panels of eight tiles along R.
+    const uint32_t live = p.kinfo != nullptr ? *p.kinfo : (uint32_t)p.K;
+    const uint32_t size_r = TO_X ? live : (uint32_t)p.N, size_l = TO_X ? (uint32_t)p.M : live;
+    const uint32_t tiles_r = (size_r + TR - 1) / TR, tiles_l = (size_l + TL - 1) / TL, tiles = tiles_r * tiles_l;
+    if (blockIdx.x >= tiles) return;
+    const uint32_t q8 = tiles >> 3, rem = tiles & 7u, x = blockIdx.x & 7u;
+    const uint32_t t = x * q8 + min(x, rem) + (blockIdx.x >> 3);
+    const uint32_t panel = t / (8 * tiles_l), width = min(8u, tiles_r - panel * 8), in_panel = t - panel * 8 * tiles_l;
+    const uint32_t r0 = (panel * 8 + in_panel % width) * TR, l0 = in_panel / width * TL;
+
+    // ---- operands on their way: 16-byte pieces of this thread
+    u32x4 piece_l[NL], piece_r[NR];
+    uint32_t block_bits[NR], block_bit = 0;   // dX: bytes of the map, and the bit that is this piece's
+    const char *row_y[NR];         // dX: rows of Y, and the map's bytes of them
+    const uint8_t *map_y[NR];
+    uint32_t at_l[NL], at_r[NR];   // byte offsets: dX of rows of dC (L); dY of the image (L) and of rows of dC (R)
+    const uint32_t dc_row = (uint32_t)p.lddc * ESZ;
+    const uint32_t slab = p.parts ? MMM_BLOCK_PARTS_BYTES : (uint32_t)(MMM_AB_ROWS * MMM_AB_COLS * ESZ);
+    const uint32_t row_l = (uint32_t)tid >> 3, c_l = (uint32_t)tid & 7u;   // pieces n of L are rows row_l + n * NT / 8, at c_l
+#pragma unroll
+    for (int n = 0; n < NL; ++n) {
+        const uint32_t row = row_l + (uint32_t)n * (NT / 8);
+        if constexpr (TO_X) {
+            at_l[n] = l0 + row < (uint32_t)p.M ? row * dc_row : OUTSIDE;
+        } else {
+            const uint32_t k = l0 + row, kb = min(k / MMM_AB_COLS, (uint32_t)p.KBA - 1u), col = k % MMM_AB_COLS;
+            at_l[n] = kb * slab;
+            if (p.parts)   // four rows of each part, behind each other in a plane
+                at_l[n] += col * MMM_PLANE_COL_BYTES + (c_l >> 2) * MMM_PLANE_BYTES + (c_l & 3u) * 8u;
+            else if (ESZ == 4)
+                at_l[n] += col * 256u + c_l * 16u;
+            else
+                at_l[n] += (c_l >> 1) * MMM_PLANE_BYTES + col * MMM_PLANE_COL_BYTES + (c_l & 1u) * 16u;
+        }
+    }
+    if constexpr (TO_X) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const uint32_t kc = r0 + row_l + (uint32_t)n * (NT / 8);
+            const bool there = kc < live;
+            const uint32_t k = p.kinfo != nullptr ? p.kmap[there ? kc : 0u] : there ? kc : 0u;
+            row_y[n] = static_cast<const char *>(p.Y) + (uint64_t)k * (uint64_t)p.ldy * ESZ;
+            map_y[n] = reinterpret_cast<const uint8_t *>(p.b_bits + (uint64_t)k * (uint64_t)p.WB);
+            at_r[n] = there ? 0xffu : 0u;   // (of the map's byte)
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const uint32_t q = (uint32_t)tid + (uint32_t)n * NT, rho = q / PIECES, col = q % PIECES * PER;
+            // the row of a step that stands at place rho of it: floats as they are have rows r, r + 16, r + 32 and r + 48 side by side in the image
+            const uint32_t row = ESZ == 4 && !p.parts ? (rho >> 2) + 16u * (rho & 3u) : rho;
+            at_r[n] = r0 + col < (uint32_t)p.N ? row * dc_row + col * ESZ : OUTSIDE;
+        }
+    }
+
+    typedef typename AnyPiece<ESZ>::type piece_any;
+    auto fetch = [&](int step) __attribute__((always_inline)) {
+        if constexpr (TO_X) {
+            const uint32_t j = (uint32_t)step * STEP + c_l * PER, N = (uint32_t)p.N;
+            const bool inside = j < N;
+            const uint32_t rows = min((uint32_t)p.M - l0, (uint32_t)TL);
+            const __amdgpu_buffer_rsrc_t dc = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<char *>(static_cast<const char *>(p.dC) + (uint64_t)l0 * dc_row), 0, (int)((rows - 1u) * dc_row + N * ESZ), 0x00020000);
+#pragma unroll
+            for (int n = 0; n < NL; ++n)
+                piece_l[n] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(dc, (int)(inside ? at_l[n] + j * ESZ : OUTSIDE), 0, 0));
+            const uint32_t jc = inside ? j : 0u, jb = jc >> p.bw_shift;   // (what exists is read, whether it counts or not)
+            block_bit = inside ? 1u << (jb & 7u) : 0u;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                piece_r[n] = *reinterpret_cast<const piece_any *>(row_y[n] + jc * ESZ);
+                block_bits[n] = (uint32_t)map_y[n][jb >> 3];
+            }
+        } else {
+            // the block of rows, and which half of it (floats)
+            const uint32_t block = ESZ == 4 ? (uint32_t)step >> 1 : (uint32_t)step, half = ESZ == 4 ? (uint32_t)step & 1u : 0u;
+            const char *const img = p.a_img + (uint64_t)block * ((uint64_t)(uint32_t)p.KBA * slab) + half * (p.parts ? 2 * MMM_PLANE_BYTES : 128u);
+#pragma unroll
+            for (int n = 0; n < NL; ++n) {
+                if (ESZ == 4 && p.parts) {
+                    u32x2 part[MMM_PARTS];
+#pragma unroll
+                    for (int q = 0; q < MMM_PARTS; ++q) part[q] = *reinterpret_cast<const u32x2 *>(img + at_l[n] + q * MMM_PART_BYTES);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        auto of = [&](int q) -> uint32_t { return part[q][u >> 1] >> (16 * (u & 1)) & 0xffffu; };
+                        const uint32_t p0 = of(0), p1 = of(1), p2 = of(2);
+                        const float sum = __uint_as_float(p0 << 16) + (__uint_as_float(p1 << 16) + __uint_as_float(p2 << 16));
+                        piece_l[n][u] = p2 == MMM_PARTS_RAW ? p0 << 16 | p1 : __float_as_uint(sum);
+                    }
+                } else {
+                    piece_l[n] = *reinterpret_cast<const u32x4 *>(img + at_l[n]);
+                }
+            }
+            const uint32_t row0 = ESZ == 4 && !p.parts ? block * 64u + half * 8u : (uint32_t)step * STEP;
+            const uint32_t left = (uint32_t)p.M > row0 ? (uint32_t)p.M - row0 : 0u;   // rows of dC from there on
+            const uint32_t cols = ((uint32_t)p.N - r0) * ESZ;
+            const __amdgpu_buffer_rsrc_t dc = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<char *>(static_cast<const char *>(p.dC) + (uint64_t)(left != 0u ? row0 : 0u) * dc_row + (uint64_t)r0 * ESZ), 0,
+                left != 0u ? (int)((min(left, 64u) - 1u) * dc_row + cols) : 0, 0x00020000);
+#pragma unroll
+            for (int n = 0; n < NR; ++n) piece_r[n] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(dc, (int)at_r[n], 0, 0));
+        }
+    };
+    // to half `to` of LDS
+    auto place = [&](int to) __attribute__((always_inline)) {
+        char *const at = lds[to];
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const uint32_t row = row_l + (uint32_t)n * (NT / 8);
+            *reinterpret_cast<u32x4 *>(at + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = piece_l[n];
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            if constexpr (TO_X) {
+                const uint32_t row = row_l + (uint32_t)n * (NT / 8);
+                u32x4 v = piece_r[n];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = (block_bits[n] & at_r[n] & block_bit) != 0u ? v[u] : 0u;
+                *reinterpret_cast<u32x4 *>(at + TL * ROWB + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = v;
+            } else {
+                const uint32_t q = (uint32_t)tid + (uint32_t)n * NT, rho = q / PIECES, col = q % PIECES;   // col: piece of the row
+                const uint32_t turned = ESZ == 4 ? ((col >> 2) ^ (rho >> 2 & 7u)) << 2 | (col & 3u) : ((col >> 1) ^ (rho & 7u)) << 1 | (col & 1u);
+                *reinterpret_cast<u32x4 *>(at + TL * ROWB + rho * TURNED_ROW + (turned << 4)) = piece_r[n];
+            }
+        }
+    };
+    floatx4 acc[FR][FL];
+#pragma unroll
+    for (int a = 0; a < FR; ++a)
+#pragma unroll
+        for (int b = 0; b < FL; ++b) acc[a][b] = floatx4{0, 0, 0, 0};
+
+    auto compute = [&](int from) __attribute__((always_inline)) {
+        const char *const at = lds[from];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            u32x4 l[FL], r[FR];
+#pragma unroll
+            for (int b = 0; b < FL; ++b) {
+                const uint32_t row = (uint32_t)((wl * FL + b) * 16 + c);
+                l[b] = *reinterpret_cast<const u32x4 *>(at + row * ROWB + (((uint32_t)(kk * 4 + s) ^ (row & 7u)) << 4));
+            }
+#pragma unroll
+            for (int a = 0; a < FR; ++a) {
+                const uint32_t col0 = (uint32_t)((wr * FR + a) * 16);
+                if constexpr (TO_X) {
+                    const uint32_t row = col0 + (uint32_t)c;
+                    r[a] = *reinterpret_cast<const u32x4 *>(at + TL * ROWB + row * ROWB + (((uint32_t)(kk * 4 + s) ^ (row & 7u)) << 4));
+                } else if constexpr (ESZ == 4) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t rho = (uint32_t)((kk * 4 + s) * 4 + u);
+                        r[a][u] = *reinterpret_cast<const uint32_t *>(at + TL * ROWB + rho * TURNED_ROW + (((col0 >> 4) ^ (rho >> 2 & 7u)) << 6) + c * 4);
+                    }
+                } else {
+                    // sixteen lanes read four rows of sixteen columns and get a column of four each
+                    typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+                    u32x2 half[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t rho = (uint32_t)((kk * 4 + s) * 8 + h * 4 + (c >> 2));
+                        const uint32_t where = TL * ROWB + rho * TURNED_ROW + (((col0 >> 4) ^ (rho & 7u)) << 5) + (uint32_t)(c & 3) * 8u;
+                        half[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)((lds_char *)lds[from] + where)));
+                    }
+                    r[a] = u32x4{half[0].x, half[0].y, half[1].x, half[1].y};
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < FR; ++a)
+#pragma unroll
+                for (int b = 0; b < FL; ++b) multiply<T>(r[a], l[b], acc[a][b]);
+        }
+    };
+    const int steps = p.steps;
+    fetch(0);
+    place(0);
+    for (int step = 0; step < steps; ++step) {
+        if (step + 1 < steps) fetch(step + 1);
+        __syncthreads();   // the step's operands are there; nobody reads the other half any more
+        compute(step & 1);
+        if (step + 1 < steps) place((step + 1) & 1);
+    }
+
+    // ---- results: a lane holds four neighbours along R of sixteen along L
+#pragma unroll
+    for (int b = 0; b < FL; ++b) {
+        const uint32_t l = l0 + (uint32_t)((wl * FL + b) * 16 + c);
+        if (l >= size_l) continue;
+        if constexpr (TO_X) {
+            const uint64_t *const bits = p.a_bits + (uint64_t)l * (uint64_t)p.WA;
+            T *const row = static_cast<T *>(p.out) + (int64_t)l * p.ldo;
+#pragma unroll
+            for (int a = 0; a < FR; ++a) {
+                const uint32_t k0 = r0 + (uint32_t)((wr * FR + a) * 16 + s * 4);
+                if (k0 >= live) continue;
+                if (p.kinfo == nullptr) {
+                    const uint32_t on = (uint32_t)(bits[k0 >> 6] >> (k0 & 63u));
+                    typedef T vec __attribute__((ext_vector_type(4)));
+                    typedef vec vec_any __attribute__((aligned(sizeof(T)), may_alias));
+                    vec v;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[u] = on >> u & 1u ? (T)acc[a][b][u] : (T)0.f;
+                    if (k0 + 4 <= live) {
+                        *reinterpret_cast<vec_any *>(row + k0) = v;
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (k0 + u < live) row[k0 + u] = v[u];
+                    }
+                } else {   // (the row holds zeros)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if (k0 + u >= live) continue;
+                        const uint32_t k = p.kmap[k0 + u];
+                        if (bits[k >> 6] >> (k & 63u) & 1ull) row[k] = (T)acc[a][b][u];
+                    }
+                }
+            }
+        } else {
+            const uint32_t k = p.kinfo != nullptr ? p.kmap[l] : l;
+            const uint64_t *const bits = p.b_bits + (uint64_t)k * (uint64_t)p.WB;
+            float *const row = static_cast<float *>(p.out) + (int64_t)k * p.ldo;
+#pragma unroll
+            for (int a = 0; a < FR; ++a) {
+                const uint32_t j = r0 + (uint32_t)((wr * FR + a) * 16 + s * 4), jb = j >> p.bw_shift;
+                if (j >= (uint32_t)p.N) continue;
+                const bool on = bits[jb >> 6] >> (jb & 63u) & 1ull;
+                typedef floatx4 vec_any __attribute__((aligned(4), may_alias));
+                vec_any *const dst = reinterpret_cast<vec_any *>(row + j);
+                if (p.accumulate) {
+                    if (on) *dst = *dst + acc[a][b];
+                } else {
+                    *dst = on ? acc[a][b] : floatx4{0, 0, 0, 0};
+                }
+            }
+        }
+    }
+}
+
+// Zeros: rows of `bytes` bytes, those of the bitmap's zero bits where there is one.  16 bytes per lane.
+__global__ __launch_bounds__(256) void mmm_clear_rows_kernel(char *out, int64_t pitch, int64_t bytes, int64_t rows, const uint64_t *kept)
+{
+    typedef AnyPiece<2>::type piece_any;
+    typedef uint16_t half_any __attribute__((may_alias));
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        if (kept != nullptr && (kept[row >> 6] >> (row & 63) & 1ull)) continue;
+        for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16; at < bytes; at += (int64_t)gridDim.x * 256 * 16) {
+            char *const to = out + row * pitch + at;
+            if (at + 16 <= bytes)
+                *reinterpret_cast<piece_any *>(to) = piece_any{0, 0, 0, 0};
+            else
+                for (int64_t q = 0; at + q < bytes; q += 2) *reinterpret_cast<half_any *>(to + q) = 0;
+        }
+    }
+}
+
+hipError_t clear_rows(void *out, int64_t pitch, int64_t bytes, int64_t rows, const uint64_t *kept, hipStream_t s)
+{
+    const dim3 grid((uint32_t)std::min<int64_t>((bytes + 4095) / 4096, 64), (uint32_t)std::min<int64_t>(rows, 65535));
+    hipLaunchKernelGGL(mmm_clear_rows_kernel, grid, dim3(256), 0, s, static_cast<char *>(out), pitch, bytes, rows, kept);
+    return hipGetLastError();
+}
+
+template <typename T, bool TO_X> hipError_t launch(const mmm_maps *m, const GradParams &p, hipStream_t s)
+{
+    constexpr int WR = 2, WL = 2, FR = 4, FL = 4;
+    const int64_t size_r = TO_X ? m->K : m->N, size_l = TO_X ? m->M : m->K;
+    const int64_t tiles = ((size_r + 16 * FR * WR - 1) / (16 * FR * WR)) * ((size_l + 16 * FL * WL - 1) / (16 * FL * WL));
+    if (tiles > (1LL << 32) / 1024 - 1) return hipErrorInvalidValue;   // threads of a launch
+    hipLaunchKernelGGL((mmm_grad_kernel<T, TO_X, WR, WL, FR, FL>), dim3((uint32_t)tiles), dim3(64 * WR * WL), 0, s, p);
+    return hipGetLastError();
+}
+
+}   // namespace
+
+hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int64_t ldy, const void *dC, int64_t lddc, void *dX, int64_t lddx, float *dY,
+                           int64_t lddy, int32_t accumulate, hipStream_t s)
+{
+    GradParams p{};
+    p.Y = Y;
+    p.ldy = ldy;
+    p.dC = dC;
+    p.lddc = lddc;
+    p.a_img = m->a_img;
+    p.a_bits = m->a_bits;
+    p.b_bits = m->b_bits;
+    p.kinfo = m->b_compact ? m->kinfo : nullptr;
+    p.kmap = m->kmap;
+    p.M = m->M;
+    p.K = m->K;
+    p.N = m->N;
+    p.WA = m->WA;
+    p.WB = m->WB;
+    p.KBA = (int32_t)m->KBA;
+    p.bw_shift = m->bw == 8 ? 3 : m->bw == 16 ? 4 : 5;
+    p.accumulate = accumulate;
+    p.parts = m->a_form == MMM_FORM_PARTS;
+    const int64_t esz = dtype == MMM_F32 ? 4 : 2;
+    (void)hipGetLastError();
+    if (dX != nullptr) {
+        if (m->b_compact)
+            if (hipError_t e = clear_rows(dX, lddx * esz, m->K * esz, m->M, nullptr, s); e != hipSuccess) return e;
+        p.out = dX;
+        p.ldo = lddx;
+        p.steps = (int32_t)((m->N * esz + ROWB - 1) / ROWB);
+        const hipError_t e = dtype == MMM_F32 ? launch<float, true>(m, p, s) : dtype == MMM_BF16 ? launch<__bf16, true>(m, p, s) : launch<_Float16, true>(m, p, s);
+        if (e != hipSuccess) return e;
+    }
+    if (dY != nullptr) {
+        if (m->b_compact && !accumulate)
+            if (hipError_t e = clear_rows(dY, lddy * 4, m->N * 4, m->K, m->rows_copy, s); e != hipSuccess) return e;
+        p.out = dY;
+        p.ldo = lddy;
+        p.steps = (int32_t)(m->MBA * (dtype == MMM_F32 ? 2 : 1));
+        return dtype == MMM_F32 ? launch<float, false>(m, p, s) : dtype == MMM_BF16 ? launch<__bf16, false>(m, p, s) : launch<_Float16, false>(m, p, s);
+    }
+    return hipSuccess;
+}

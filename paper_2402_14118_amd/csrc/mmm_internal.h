@@ -346,3 +346,6 @@ hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_bl
 size_t mmm_epilogue_grad_bytes(int64_t M, int64_t N);
 hipError_t mmm_launch_epilogue_grad(int64_t M, int64_t N, int32_t dt, int32_t out_dtype, int32_t activation, const void *dC, int64_t lddc, const void *Z,
                                     int64_t ldz, void *dZ, int64_t lddz, float *dbias, void *workspace, hipStream_t s);
+// gradients of the product: dX and dY, either may be null
+hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int64_t ldy, const void *dC, int64_t lddc, void *dX, int64_t lddx, float *dY,
+                           int64_t lddy, int32_t accumulate, hipStream_t s);

@@ -143,3 +143,20 @@ def test_the_engine_checks_tensors_of_the_epilogue():
     with pytest.raises(mm.MmmError) as e:
         eng.matmul_epilogue(X, Y, C, stream=0)
     assert e.value.status == B.MMM_ERR_INVALID_ARG
+
+
+def test_matmul_backward_refuses():
+    need = mm.mmm_maps_workspace_bytes(64, 128, 64, 16)
+    maps = mm.mmm_maps_init(AT, need, 64, 128, 64, 16)
+
+    def call(handle=maps, dt=1, X=at(1), ldx=128, Y=at(2), ldy=64, dC=at(3), lddc=64, dX=at(4), lddx=128, dY=at(5), lddy=64):
+        return B.lib.mmm_matmul_backward(handle, dt, X, ldx, Y, ldy, dC, lddc, dX, lddx, dY, lddy, 0, None)
+    try:
+        assert call() == call(dX=None, lddx=0) == call(dY=None, lddy=0) == B.MMM_ERR_MAPS_MISMATCH
+        for missing in (dict(handle=None), dict(X=None), dict(Y=None), dict(dC=None), dict(dX=None, dY=None)):
+            assert call(**missing) == B.MMM_ERR_INVALID_ARG
+        assert call(dt=3) == call(dt=4) == call(X=at(1) + 1) == call(dC=at(3) + 1) == call(dX=at(4) + 1) == call(dY=at(5) + 2) == B.MMM_ERR_DTYPE
+        for short in (dict(ldx=127), dict(ldy=63), dict(lddc=63), dict(lddx=127), dict(lddy=63), dict(lddc=1 << 22)):
+            assert call(**short) == B.MMM_ERR_SHAPE
+    finally:
+        mm.mmm_maps_release(maps)

@@ -1,0 +1,153 @@
+"""The gradients of the masked product against the formulas in 64 bits, under the maps as built.
+
+Bound: a float sum of n products of exact operands is off by at most n roundings of 2^-24 of the sum of their magnitudes, whatever the order
+(floats: and one for the product); n is the length of the contraction here, at most 2048.  dX is rounded to its type once more.  Small whole numbers are exact."""
+import pytest
+import torch
+
+import paper_2402_14118_amd as mm
+from test_gpu_matmul_epilogue import T, room, words
+
+U = 2.0 ** -24
+
+
+class Problem:
+    def __init__(self, M, K, N, bw, dt, p_a=0.3, p_b=0.5, p_rows=None, pad=0, whole=False, seed=0):
+        self.M, self.K, self.N, self.bw, self.dt = M, K, N, bw, dt
+        g = torch.Generator().manual_seed(seed + 3 * M + 5 * K + 7 * N)
+        t = T[dt][1]
+
+        def values(r, c):
+            v = torch.randint(-3, 4, (r, c), generator=g).float() if whole else torch.randn(r, c, generator=g)
+            return v.to(t)
+        X, Y, dC = values(M, K), values(K, N), values(M, N)
+        keep = torch.rand(M, K, generator=g) < p_a
+        blocks = torch.rand(K, N // bw, generator=g) < p_b
+        if M > 3:
+            keep[2] = False
+        if K > 3:
+            blocks[1] = False
+        rows = None if p_rows is None else torch.rand(1, K, generator=g) < p_rows
+        on = (blocks if rows is None else blocks & rows.view(-1, 1)) & (Y.view(K, -1, bw) != 0).any(2)
+        self.a_on, self.b_on = keep & (X != 0), on.repeat_interleave(bw, 1)
+        self.A, self.B, self.G = X.double() * self.a_on, Y.double() * self.b_on, dC.double()
+        # what is masked out may hold anything
+        X[~keep] = float("nan")
+        Y[~(blocks if rows is None else blocks & rows.view(-1, 1)).repeat_interleave(bw, 1)] = float("inf")
+        self.X, self.Y, self.dC = (room(*v.shape, t, pad, 1 if pad else 0)[1].copy_(v.cuda()) for v in (X, Y, dC))
+        self.dXall, self.dX = room(M, K, t, pad, 1 if pad else 0)
+        self.dYall, self.dY = room(K, N, torch.float32, pad, 1 if pad else 0)
+        self.eng = mm.MaskedMatmul(M, K, N, bw, T[dt][0])
+        self.eng.build_maps(self.X, self.Y, keep_a=words(keep), keep_rows=None if rows is None else words(rows), keep_blocks=words(blocks))
+
+    def check(self, exact=False):
+        self.dXall.fill_(77.0)
+        self.dYall.fill_(77.0)
+        self.eng.matmul_backward(self.X, self.Y, self.dC, self.dX, self.dY)
+        half = torch.finfo(self.dX.dtype).eps / 2
+        want = (self.G @ self.B.t()) * self.a_on, (self.A.t() @ self.G) * self.b_on
+        mags = self.G.abs() @ self.B.abs().t(), self.A.abs().t() @ self.G.abs()
+        for what, got, w, mag, n, step in (("dX", self.dX, want[0], mags[0], self.N, half), ("dY", self.dY, want[1], mags[1], self.M, 0.0)):
+            err = (got.double().cpu() - w).abs()
+            bound = torch.zeros_like(err) if exact else (n + 1) * U * mag + step * w.abs() * (1 + 1e-3)
+            if exact and self.dt != "f32" and what == "dX":
+                bound = step * w.abs()
+            assert bool((err <= bound).all()), (what, float(err.max()), int((~(err <= bound)).sum()))
+        assert bool((self.dX.cpu()[~self.a_on] == 0).all()) and bool((self.dY.cpu()[~self.b_on] == 0).all())
+        first, sums = self.dX.clone(), self.dY.clone()
+        # added to; one of the two alone; the same again
+        self.dY.fill_(1.0)
+        self.eng.matmul_backward(self.X, self.Y, self.dC, dY=self.dY, accumulate=True)
+        assert torch.equal(self.dY, sums + 1.0)
+        self.dX.fill_(5.0)
+        self.eng.matmul_backward(self.X, self.Y, self.dC, dX=self.dX)
+        assert torch.equal(self.dX, first)
+        for whole, t in ((self.dXall, self.dX), (self.dYall, self.dY)):
+            t.fill_(77.0)
+            assert bool((whole == 77.0).all()), "outside"
+
+
+SHAPES = [(1, 1, 8, 8), (3, 7, 16, 16), (17, 130, 40, 8), (64, 128, 128, 16), (65, 129, 136, 8), (200, 333, 264, 8), (129, 1000, 160, 32), (300, 257, 1056, 32)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [None, 0.3])
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("M,K,N,bw", SHAPES)
+def test_gradients(M, K, N, bw, dt, rows):
+    Problem(M, K, N, bw, dt, p_rows=rows, pad=3 if M % 2 else 0).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+def test_whole_numbers_are_exact(dt):
+    Problem(150, 300, 200, 8, dt, whole=True).check(exact=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [None, 0.4])
+def test_floats_in_parts(rows):
+    """The image of A in three parts, among them elements that parts do not hold."""
+    mm.mmm_set_option("float_form", 1)
+    try:
+        p = Problem(200, 300, 264, 8, "f32", p_rows=rows)
+        assert mm.mmm_matmul_form(p.eng.maps) == 1
+        p.check()
+        at = p.a_on.nonzero()[5]
+        X = p.X.clone()
+        X[at[0], at[1]] = 2.0 ** 60
+        p.A[at[0], at[1]] = 2.0 ** 60
+        p.eng.build_maps(X, None, keep_a=words(p.a_on))
+        p.X = X
+        p.check()
+    finally:
+        mm.mmm_set_option("float_form", -1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("p_rows", [0.0, 1.0])
+def test_all_or_none(dt, p_rows):
+    """No live row at all (both gradients are zero), and all of them."""
+    Problem(70, 200, 64, 16, dt, p_rows=p_rows).check()
+    Problem(70, 200, 64, 16, dt, p_a=0.0).check()
+    Problem(70, 200, 64, 16, dt, p_a=1.0, p_b=1.0).check()
+
+
+@pytest.mark.gpu
+def test_gradients_against_differences():
+    """Along random directions of the kept elements the product is linear in each operand: C(X + e) - C(X) is the slope itself but for rounding, 300
+    roundings of 2^-24 of the sum of magnitudes."""
+    p = Problem(40, 300, 96, 16, "f32")
+    p.eng.matmul_backward(p.X, p.Y, p.dC, p.dX, p.dY)
+    g = torch.Generator().manual_seed(3)
+    wx, wy = torch.randn(40, 300, generator=g).double() * p.a_on, torch.randn(300, 96, generator=g).double() * p.b_on
+    for grad, along, change in ((p.dX, wx, wx @ p.B), (p.dY, wy, p.A @ wy)):
+        terms = grad.double().cpu() * along
+        assert abs(float((p.G * change).sum()) - float(terms.sum())) <= 300 * U * float((p.G.abs() @ p.B.abs().t() * along.abs()).sum() if grad is p.dX
+                                                                                      else (p.A.abs().t() @ p.G.abs() * along.abs()).sum())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [None, 0.3])
+def test_another_stream_and_a_replayed_graph(rows):
+    p = Problem(130, 400, 200, 8, "bf16", p_rows=rows)
+    p.eng.matmul_backward(p.X, p.Y, p.dC, p.dX, p.dY)
+    want = p.dX.clone(), p.dY.clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        p.dX.fill_(3.0)
+        p.dY.fill_(3.0)
+        p.eng.matmul_backward(p.X, p.Y, p.dC, p.dX, p.dY)
+    side.synchronize()
+    assert torch.equal(p.dX, want[0]) and torch.equal(p.dY, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.eng.matmul_backward(p.X, p.Y, p.dC, p.dX, p.dY)
+    for _ in range(3):
+        p.dX.fill_(3.0)
+        p.dY.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(p.dX, want[0]) and torch.equal(p.dY, want[1])
