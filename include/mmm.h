@@ -398,7 +398,8 @@ mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype o
 /* The gradients of the product A x B under the maps as built (which are held fixed):
  *     dX[i,k] = a_bits[i,k] ? sum over j with b_bits[k, j div bw] of dC[i,j] Y[k,j] : 0
  *     dY[k,j] = b_bits[k, j div bw] ? sum over i with a_bits[i,k] of X[i,k] dC[i,j] : 0
- * A zero element of X and a block of Y that holds only zeros thus get none.  X, Y, dC (M x lddc) and dX have type dt; dY is float. dX or dY may
+ * A zero element of X and a block of Y that holds only zeros thus get none: all_x != 0 asks for dX at every element (an X whose zeros are values
+ * like others, where the mask only saves work); a block of weights has to start from something.  X, Y, dC (M x lddc) and dX have type dt; dY is float. dX or dY may
  * be NULL (not both).  accumulate != 0: dY += instead (unoccupied blocks stay as they are).  dX and dY overlap no input.
  * X must be the one the A side was built from (address, ldx); the Y given is what is read, under the maps as built.
  * Masked-out elements of X and unoccupied blocks of Y never reach the arithmetic, whatever they hold.  Elements of dC are expected
@@ -408,7 +409,7 @@ mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype o
  * mmm_matmul), MMM_ERR_DEVICE. */
 mmm_status mmm_matmul_backward(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y, int64_t ldy,
                                const void *dC, int64_t lddc, void *dX, int64_t lddx, float *dY, int64_t lddy,
-                               int32_t accumulate, void *hip_stream);
+                               int32_t accumulate, int32_t all_x, void *hip_stream);
 
 /* The norms around a block.  For every row i of N elements:
  *     v  = norm_post(y) * post_weight + post_bias          (post == MMM_NORM_NONE: v = y)

@@ -6,5 +6,5 @@ owns the device buffers of one problem.
 """
 from .binding import *          # noqa: F401,F403
 from .binding import BlockNormDesc, BlockNormGrads, Epilogue, MaskA, MaskB, MmmError, lib, LIB_PATH, EXPORTS   # noqa: F401
-from .block import BlockNorm                                         # noqa: F401
+from .block import BlockNorm, MaskedMlp                              # noqa: F401
 from .engine import MaskedMatmul                                     # noqa: F401

@@ -108,7 +108,7 @@ def _load() -> ctypes.CDLL:
     lib.mmm_matmul_variant_name.restype = c.c_char_p
     lib.mmm_matmul_plan.argtypes = [vp, i32, c.POINTER(i32), c.POINTER(i32), c.POINTER(i64)]
     lib.mmm_matmul_epilogue.argtypes = [vp, i32, vp, i64, c.POINTER(MaskA), vp, i64, vp, i64, c.POINTER(Epilogue), vp]
-    lib.mmm_matmul_backward.argtypes = [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp]
+    lib.mmm_matmul_backward.argtypes = [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp]
     lib.mmm_epilogue_backward_workspace_bytes.argtypes = [i64, i64, c.POINTER(c.c_size_t)]
     lib.mmm_epilogue_backward.argtypes = [i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, c.c_size_t, vp]
     lib.mmm_block_norm.argtypes = [c.POINTER(BlockNormDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp]
@@ -313,8 +313,8 @@ def mmm_matmul_epilogue(maps: int, dt: int, X, ldx: int, ma: Optional[MaskA], Y,
 
 
 def mmm_matmul_backward(maps: int, dt: int, X, ldx: int, Y, ldy: int, dC, lddc: int, dX, lddx: int, dY, lddy: int, accumulate: int = 0,
-                        stream=None) -> None:
-    _check(lib.mmm_matmul_backward(maps, dt, _ptr(X), ldx, _ptr(Y), ldy, _ptr(dC), lddc, _ptr(dX), lddx, _ptr(dY), lddy, int(accumulate),
+                        all_x: int = 0, stream=None) -> None:
+    _check(lib.mmm_matmul_backward(maps, dt, _ptr(X), ldx, _ptr(Y), ldy, _ptr(dC), lddc, _ptr(dX), lddx, _ptr(dY), lddy, int(accumulate), int(all_x),
                                    _stream(stream)), "mmm_matmul_backward")
 
 

@@ -10,7 +10,8 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from .tensors import check_device, own_device, rows
+from .engine import MaskedMatmul
+from .tensors import TORCH_TYPES, check_device, own_device, rows
 
 
 class BlockNorm:
@@ -77,3 +78,96 @@ class BlockNorm:
                              p(self._vector("grad_post_bias", grad_post_bias, f)), p(self._vector("grad_pre_weight", grad_pre_weight, f)),
                              p(self._vector("grad_pre_bias", grad_pre_bias, f)))
         B.mmm_block_norm_backward(d, g, self.workspace, 0 if self.workspace is None else self.workspace.numel(), stream)
+
+
+class MaskedMlp:
+    """A residual MLP block on masked products, from the norm in front of it to the norm in front of the next one:
+
+        a  = act(N x W1 + b1)                        N: the normed stream, M x width
+        y  = M(a) x W2 + b2                          what the activation leaves at zero is skipped
+        h' = alpha H + gate norm(y),  n' = norm(h')
+
+    W1 (width x hidden) and W2 (hidden x width) are masked in blocks of their rows (a block that holds only zeros is off, and learns nothing); rows of W2 (hidden units) may be selected by context.  The
+    holder owns the maps of both products, the activations between them and, with training=True, the gradients on the way and the
+    workspaces of backward(): two calls that may run at the same time need a holder each.  fused (few rows, not for training): both products
+    evaluate their masks themselves, one launch each."""
+
+    def __init__(self, M: int, width: int, hidden: int, block_width: int = 32, dtype: int = B.MMM_BF16, activation: int = B.MMM_ACT_RELU,
+                 post: int = B.MMM_NORM_RMS, pre: int = B.MMM_NORM_RMS, gate: int = B.MMM_GATE_NONE, alpha: float = 1.0, eps: float = 1e-5,
+                 dtype_h: Optional[int] = None, fused: bool = False, training: bool = False, device="cuda:0"):
+        if fused and training:
+            raise ValueError("the gradients need the maps of the activations, which fused products do not make")
+        self.M, self.width, self.hidden, self.dtype, self.activation, self.fused, self.training = M, width, hidden, dtype, activation, fused, training
+        self.device = own_device(device)
+        self.up = MaskedMatmul(M, width, hidden, block_width, dtype, self.device)
+        self.down = MaskedMatmul(M, hidden, width, block_width, dtype, self.device)
+        self.norm = BlockNorm(M, width, dtype, post, pre, gate, alpha, eps, dtype_h, training=training, device=self.device)
+        # zeros of ReLU are told by the sign, those of a smooth activation by the value
+        self.pred = B.MMM_PRED_GT if activation == B.MMM_ACT_RELU else B.MMM_PRED_NONZERO
+
+        def room(*shape, t=None):
+            return torch.empty(shape, dtype=TORCH_TYPES[dtype if t is None else t], device=self.device)
+        self.a, self.y = room(M, hidden), room(M, width)
+        # what the slope is taken at: ReLU's is told by its value
+        self.preact = self.a if activation in (B.MMM_ACT_RELU, B.MMM_ACT_NONE) else room(M, hidden) if training else None
+        self.W1 = self.b1 = self.W2 = self.b2 = None
+        if training:
+            self.grad_a, self.grad_y = room(M, hidden), room(M, width)
+            nbytes = max(B.mmm_epilogue_backward_workspace_bytes(M, n) for n in (hidden, width))
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def close(self) -> None:
+        self.up.close()
+        self.down.close()
+
+    def set_weights(self, W1: torch.Tensor, W2: torch.Tensor, b1: Optional[torch.Tensor] = None, b2: Optional[torch.Tensor] = None,
+                    keep_blocks1: Optional[torch.Tensor] = None, keep_blocks2: Optional[torch.Tensor] = None,
+                    keep_rows2: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Build the maps of both weights; again after a weight or a selection has changed."""
+        check_device(self.device)
+        rows("W1", W1, (self.width, self.hidden), self.dtype, self.device, False)
+        rows("W2", W2, (self.hidden, self.width), self.dtype, self.device, False)
+        self.W1, self.W2, self.b1, self.b2 = W1, W2, b1, b2
+        self.up.build_maps(None, W1, keep_blocks=keep_blocks1, stream=stream)
+        self.down.build_maps(None, W2, keep_rows=keep_rows2, keep_blocks=keep_blocks2, stream=stream)
+
+    def _product(self, eng, X, Y, C, pred, stream, **epilogue):
+        if self.fused:
+            eng.matmul_epilogue(X, Y, C, pred=pred, stream=stream, **epilogue)
+        else:
+            eng.build_maps(X, None, pred, stream=stream)
+            eng.matmul_epilogue(X, Y, C, stream=stream, **epilogue)
+
+    def forward(self, N: torch.Tensor, H: torch.Tensor, H_out: torch.Tensor, normed: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None, pre_weight: Optional[torch.Tensor] = None,
+                pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
+        """H_out may be H (backward() does not need H); normed receives n'."""
+        if self.W1 is None:
+            raise ValueError("set_weights() comes first")
+        rows("N", N, (self.M, self.width), self.dtype, self.device, False)
+        kept = self.preact if self.training and self.preact is not self.a else None
+        self._product(self.up, N, self.W1, self.a, B.MMM_PRED_NONZERO, stream, bias=self.b1, activation=self.activation, preact=kept)
+        self._product(self.down, self.a, self.W2, self.y, self.pred, stream, bias=self.b2)
+        self.norm.forward(H, normed=normed, H_out=H_out, Y=self.y, gate=gate, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight,
+                          pre_bias=pre_bias, stream=stream)
+
+    def backward(self, N: torch.Tensor, H_out: torch.Tensor, grad_N: torch.Tensor, grad_H: torch.Tensor, grad_normed: Optional[torch.Tensor] = None,
+                 grad_H_out: Optional[torch.Tensor] = None, grad_W1: Optional[torch.Tensor] = None, grad_W2: Optional[torch.Tensor] = None,
+                 grad_b1: Optional[torch.Tensor] = None, grad_b2: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None, **norm) -> None:
+        """The gradients of the forward call before it (N as it was then, H_out as it left it).  grad_W1, grad_W2, grad_b1, grad_b2 are float;
+        accumulate: those of the weights are added to.  norm: the values (gate, post_weight, post_bias, pre_weight) and gradients (grad_gate,
+        grad_post_weight, grad_post_bias, grad_pre_weight, grad_pre_bias) of BlockNorm.backward."""
+        if not self.training:
+            raise ValueError("made without training=True")
+        M, ws, od = self.M, self.workspace, self.dtype
+        self.norm.backward(H_out=H_out, grad_normed=grad_normed, grad_H_out=grad_H_out, grad_H=grad_H, Y=self.y, grad_Y=self.grad_y, stream=stream, **norm)
+        if grad_b2 is not None:
+            rows("grad_b2", grad_b2, (self.width,), B.MMM_F32, self.device)
+            B.mmm_epilogue_backward(M, self.width, od, od, B.MMM_ACT_NONE, self.grad_y, self.width, None, 0, None, 0, grad_b2, ws, ws.numel(), stream)
+        # (a unit that ReLU has turned off has no slope; elsewhere a zero is a value like others)
+        self.down.matmul_backward(self.a, self.W2, self.grad_y, dX=self.grad_a, dY=grad_W2, accumulate=accumulate,
+                                  all_x=self.activation != B.MMM_ACT_RELU, stream=stream)
+        rows("grad_b1", grad_b1, (self.hidden,), B.MMM_F32, self.device)
+        B.mmm_epilogue_backward(M, self.hidden, od, od, self.activation, self.grad_a, self.hidden, self.preact, self.hidden, self.grad_a, self.hidden,
+                                grad_b1, ws, ws.numel(), stream)
+        self.up.matmul_backward(N, self.W1, self.grad_a, dX=grad_N, dY=grad_W1, accumulate=accumulate, all_x=True, stream=stream)

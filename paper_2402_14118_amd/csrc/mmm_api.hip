@@ -1059,7 +1059,7 @@ mmm_status mmm_block_norm_backward(const mmm_block_norm_desc *desc, const mmm_bl
 }
 
 mmm_status mmm_matmul_backward(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y, int64_t ldy, const void *dC,
-                               int64_t lddc, void *dX, int64_t lddx, float *dY, int64_t lddy, int32_t accumulate, void *hip_stream)
+                               int64_t lddc, void *dX, int64_t lddx, float *dY, int64_t lddy, int32_t accumulate, int32_t all_x, void *hip_stream)
 {
     if (maps == nullptr || X == nullptr || Y == nullptr || dC == nullptr || (dX == nullptr && dY == nullptr)) return MMM_ERR_INVALID_ARG;
     if (!trains(dt)) return MMM_ERR_DTYPE;
@@ -1068,7 +1068,7 @@ mmm_status mmm_matmul_backward(const mmm_maps *maps, mmm_dtype dt, const void *X
     if (!placed(X, dt) || !placed(Y, dt) || !placed(dC, dt) || !placed(dX, dt) || !placed(dY, MMM_F32)) return MMM_ERR_DTYPE;
     if (!maps->a_built || !maps->b_built || maps->a_dtype != dt || maps->b_dtype != dt) return MMM_ERR_MAPS_MISMATCH;
     if (maps->a_src != X || maps->a_src_ld != ldx) return MMM_ERR_MAPS_MISMATCH;   // the values of A are those of the image
-    if (hipError_t e = mmm_launch_grad(maps, dt, Y, ldy, dC, lddc, dX, lddx, dY, lddy, accumulate ? 1 : 0, static_cast<hipStream_t>(hip_stream));
+    if (hipError_t e = mmm_launch_grad(maps, dt, Y, ldy, dC, lddc, dX, lddx, dY, lddy, accumulate ? 1 : 0, all_x ? 1 : 0, static_cast<hipStream_t>(hip_stream));
         e != hipSuccess) {
         note_device_error("product gradient launch", e);
         return MMM_ERR_DEVICE;

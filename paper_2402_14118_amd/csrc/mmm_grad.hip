@@ -267,14 +267,14 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
         const uint32_t l = l0 + (uint32_t)((wl * FL + b) * 16 + c);
         if (l >= size_l) continue;
         if constexpr (TO_X) {
-            const uint64_t *const bits = p.a_bits + (uint64_t)l * (uint64_t)p.WA;
+            const uint64_t *const bits = p.a_bits != nullptr ? p.a_bits + (uint64_t)l * (uint64_t)p.WA : nullptr;   // null: all elements are wanted
             T *const row = static_cast<T *>(p.out) + (int64_t)l * p.ldo;
 #pragma unroll
             for (int a = 0; a < FR; ++a) {
                 const uint32_t k0 = r0 + (uint32_t)((wr * FR + a) * 16 + s * 4);
                 if (k0 >= live) continue;
                 if (p.kinfo == nullptr) {
-                    const uint32_t on = (uint32_t)(bits[k0 >> 6] >> (k0 & 63u));
+                    const uint32_t on = bits != nullptr ? (uint32_t)(bits[k0 >> 6] >> (k0 & 63u)) : 0xfu;
                     typedef T vec __attribute__((ext_vector_type(4)));
                     typedef vec vec_any __attribute__((aligned(sizeof(T)), may_alias));
                     vec v;
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
                     for (int u = 0; u < 4; ++u) {
                         if (k0 + u >= live) continue;
                         const uint32_t k = p.kmap[k0 + u];
-                        if (bits[k >> 6] >> (k & 63u) & 1ull) row[k] = (T)acc[a][b][u];
+                        if (bits == nullptr || (bits[k >> 6] >> (k & 63u) & 1ull)) row[k] = (T)acc[a][b][u];
                     }
                 }
             }
@@ -354,7 +354,7 @@ template <typename T, bool TO_X> hipError_t launch(const mmm_maps *m, const Grad
 }   // namespace
 
 hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int64_t ldy, const void *dC, int64_t lddc, void *dX, int64_t lddx, float *dY,
-                           int64_t lddy, int32_t accumulate, hipStream_t s)
+                           int64_t lddy, int32_t accumulate, int32_t all_x, hipStream_t s)
 {
     GradParams p{};
     p.Y = Y;
@@ -362,7 +362,7 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
     p.dC = dC;
     p.lddc = lddc;
     p.a_img = m->a_img;
-    p.a_bits = m->a_bits;
+    p.a_bits = all_x ? nullptr : m->a_bits;
     p.b_bits = m->b_bits;
     p.kinfo = m->b_compact ? m->kinfo : nullptr;
     p.kmap = m->kmap;

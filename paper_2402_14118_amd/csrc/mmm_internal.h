@@ -348,4 +348,4 @@ hipError_t mmm_launch_epilogue_grad(int64_t M, int64_t N, int32_t dt, int32_t ou
                                     int64_t ldz, void *dZ, int64_t lddz, float *dbias, void *workspace, hipStream_t s);
 // gradients of the product: dX and dY, either may be null
 hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int64_t ldy, const void *dC, int64_t lddc, void *dX, int64_t lddx, float *dY,
-                           int64_t lddy, int32_t accumulate, hipStream_t s);
+                           int64_t lddy, int32_t accumulate, int32_t all_x, hipStream_t s);

@@ -80,13 +80,13 @@ class MaskedMatmul:
                                           B._stream(stream)), "mmm_matmul_epilogue")
 
     def matmul_backward(self, X: torch.Tensor, Y: torch.Tensor, dC: torch.Tensor, dX: Optional[torch.Tensor] = None,
-                        dY: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
-        """The gradients of A x B under the maps as built: dX (type of X; zero where A is) and dY (float; zero where B has no block, or
-        added to).  X must be the tensor the maps were built from."""
+                        dY: Optional[torch.Tensor] = None, accumulate: bool = False, all_x: bool = False, stream=None) -> None:
+        """The gradients of A x B under the maps as built: dX (type of X; zero where A is, unless all_x asks for every element) and dY (float;
+        zero where B has no block, or added to).  X must be the tensor the maps were built from."""
         check_device(self.device)
         dev, dt, mk, kn = self.device, self.dtype, (self.M, self.K), (self.K, self.N)
         B.mmm_matmul_backward(self.maps, dt, *rows("X", X, mk, dt, dev, False), *rows("Y", Y, kn, dt, dev, False), *rows("dC", dC, (self.M, self.N), dt, dev, False),
-                              *rows("dX", dX, mk, dt, dev), *rows("dY", dY, kn, B.MMM_F32, dev), accumulate, stream)
+                              *rows("dX", dX, mk, dt, dev), *rows("dY", dY, kn, B.MMM_F32, dev), accumulate, all_x, stream)
 
     def set_path(self, path: int = -1) -> None:
         B.mmm_maps_set_path(self.maps, path)

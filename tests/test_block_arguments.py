@@ -150,7 +150,7 @@ def test_matmul_backward_refuses():
     maps = mm.mmm_maps_init(AT, need, 64, 128, 64, 16)
 
     def call(handle=maps, dt=1, X=at(1), ldx=128, Y=at(2), ldy=64, dC=at(3), lddc=64, dX=at(4), lddx=128, dY=at(5), lddy=64):
-        return B.lib.mmm_matmul_backward(handle, dt, X, ldx, Y, ldy, dC, lddc, dX, lddx, dY, lddy, 0, None)
+        return B.lib.mmm_matmul_backward(handle, dt, X, ldx, Y, ldy, dC, lddc, dX, lddx, dY, lddy, 0, 0, None)
     try:
         assert call() == call(dX=None, lddx=0) == call(dY=None, lddy=0) == B.MMM_ERR_MAPS_MISMATCH
         for missing in (dict(handle=None), dict(X=None), dict(Y=None), dict(dC=None), dict(dX=None, dY=None)):

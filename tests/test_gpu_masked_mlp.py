@@ -1,0 +1,118 @@
+"""The operators together: a residual MLP block, forward and backward, against the same block in 64 bits and its automatic differentiation.
+
+Floats.  Each of the eight steps errs by at most 130 roundings of 2^-24 (sums of at most 128 terms) of the magnitudes it adds, 7.8e-6; the
+magnitudes are up to sqrt(128) times the results (random signs): 8 * 7.8e-6 * 12 = 7.5e-4 of the largest value of an output at most.  No argument
+of ReLU lies within 1e-4 of zero, so that no error turns a unit on or off.  bf16: a step rounds its output by 2^-9 at most; eight of them,
+amplified the same, stay below .19 of the largest value; the 2-norm, where they add up as random numbers, below .05."""
+import pytest
+import torch
+
+import paper_2402_14118_amd as mm
+from test_gpu_matmul_epilogue import T, words
+
+EPS = 1e-5
+
+
+def standard(x, layer):
+    x = x - x.mean(1, keepdim=True) if layer else x
+    return x / (x.pow(2).mean(1, keepdim=True) + EPS).sqrt()
+
+
+def block(p, act, on1, on2):
+    a = p["N"] @ (p["W1"] * on1) + p["b1"]
+    z = a
+    a = {"relu": torch.relu, "silu": torch.nn.functional.silu}[act](a)
+    y = a @ (p["W2"] * on2) + p["b2"]
+    h = 0.9 * p["H"] + p["gate"] * (standard(y, False) * p["post_weight"])
+    return z, h, standard(h, True) * p["pre_weight"] + p["pre_bias"]
+
+
+def setup(dt, act, M=40, d=64, f=128, context=True, **how):
+    g = torch.Generator().manual_seed(11)
+    t = T[dt][1]
+    shapes = dict(N=((M, d), 1.0, 0.0), W1=((d, f), 0.15, 0.0), b1=((f,), 0.3, -0.5), W2=((f, d), 0.1, 0.0), b2=((d,), 0.1, 0.0), H=((M, d), 1.0, 0.0),
+                  gate=((d,), 0.3, 0.5), post_weight=((d,), 0.1, 1.0), pre_weight=((d,), 0.1, 1.0), pre_bias=((d,), 0.1, 0.0))
+    host = {k: (torch.randn(s, generator=g) * std + mean).to(t) for k, (s, std, mean) in shapes.items()}
+    k1, k2, r2 = torch.rand(d, f // 16, generator=g) < 0.7, torch.rand(f, d // 16, generator=g) < 0.8, torch.rand(1, f, generator=g) < 0.5
+    on1 = k1.repeat_interleave(16, 1)
+    on2 = k2.repeat_interleave(16, 1) & (r2.view(-1, 1) if context else True)
+    dev = {k: v.cuda() for k, v in host.items()}
+    mlp = mm.MaskedMlp(M, d, f, 16, T[dt][0], mm.MMM_ACT_RELU if act == "relu" else mm.MMM_ACT_SILU, mm.MMM_NORM_RMS, mm.MMM_NORM_LAYER, mm.MMM_GATE_COL, 0.9, EPS, **how)
+    mlp.set_weights(dev["W1"], dev["W2"], dev["b1"], dev["b2"], words(k1), words(k2), words(r2) if context else None)
+    return mlp, dev, {k: v.double().requires_grad_() for k, v in host.items()}, on1.double(), on2.double()
+
+
+def close(got, want, dt, what):
+    err = (got.double().cpu() - want).abs()
+    limit = (7.5e-4 if dt == "f32" else 0.19) * float(want.abs().max())
+    assert float(err.max()) <= limit, (what, float(err.max()), limit)
+    if dt != "f32":
+        assert float(err.norm()) <= 0.05 * float(want.norm()), (what, float(err.norm() / want.norm()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,act,context", [("f32", "relu", True), ("f32", "silu", False), ("bf16", "silu", True), ("f16", "relu", False)])
+def test_training_step(dt, act, context):
+    mlp, d, ref, on1, on2 = setup(dt, act, context=context, training=True)
+    values = {k: d[k] for k in ("gate", "post_weight", "pre_weight")}
+    H_out, n = torch.empty_like(d["H"]), torch.empty_like(d["H"])
+    mlp.forward(d["N"], d["H"], H_out, n, pre_bias=d["pre_bias"], **values)
+    z, h, want_n = block(ref, act, on1, on2)
+    if act == "relu" and dt == "f32":
+        assert float(z.detach().abs().min()) > 1e-4
+    close(H_out, h.detach(), dt, "H_out")
+    close(n, want_n.detach(), dt, "n")
+    g = torch.Generator().manual_seed(4)
+    up_n, up_h = (torch.randn(h.shape, generator=g).to(T[dt][1]) for _ in range(2))
+    ((want_n * up_n.double()).sum() + (h * up_h.double()).sum()).backward()
+
+    def grads():
+        out = {"grad_N": torch.empty_like(d["N"]), "grad_H": torch.empty_like(d["H"]), **{"grad_" + k: torch.full(d[k].shape, float("nan"), device="cuda")
+               for k in ("W1", "W2", "b1", "b2", "gate", "post_weight", "pre_weight", "pre_bias")}}
+        mlp.backward(d["N"], H_out, grad_normed=up_n.cuda(), grad_H_out=up_h.cuda(), **values, **out)
+        return out
+    out = grads()
+    for k, v in out.items():
+        close(v, ref[k[5:]].grad, dt, k)
+    # a step captured into a graph, replayed with the program's own step between replays
+    torch.cuda.synchronize()
+    un, uh = up_n.cuda(), up_h.cuda()
+    again = {k: torch.empty_like(v) for k, v in out.items()}
+    H2, n2 = torch.empty_like(H_out), torch.empty_like(n)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mlp.forward(d["N"], d["H"], H2, n2, pre_bias=d["pre_bias"], **values)
+        mlp.backward(d["N"], H2, grad_normed=un, grad_H_out=uh, **values, **again)
+    for _ in range(3):
+        for t in (H2, n2, *again.values()):
+            t.fill_(0.0)
+        mlp.forward(d["N"], d["H"], H_out, n, pre_bias=d["pre_bias"], **values)
+        eager = grads()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(H2, H_out) and torch.equal(n2, n)
+        assert all(torch.equal(eager[k], again[k]) and torch.equal(eager[k], out[k]) for k in out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 5])
+def test_decode(M):
+    """Few rows: masks evaluated inside the products, the stream in place and in float beside 16-bit weights."""
+    mlp, d, ref, on1, on2 = setup("bf16", "relu", M=M, context=False, fused=True, dtype_h=mm.MMM_F32)
+    stream, n = d["H"].float(), torch.empty_like(d["N"])
+    mlp.forward(d["N"], stream, stream, n, gate=d["gate"], post_weight=d["post_weight"], pre_weight=d["pre_weight"], pre_bias=d["pre_bias"])
+    _, h, want_n = block(ref, "relu", on1, on2)
+    close(stream, h.detach(), "bf16", "H_out")
+    close(n, want_n.detach(), "bf16", "n")
+
+
+@pytest.mark.gpu
+def test_order_of_calls():
+    mlp, d, *_ = setup("bf16", "relu")
+    out = torch.empty_like(d["H"])
+    with pytest.raises(ValueError):
+        mlp.backward(d["N"], out, out, out)
+    with pytest.raises(ValueError):
+        mm.MaskedMlp(4, 64, 64, fused=True, training=True)
+    with pytest.raises(ValueError):
+        mm.MaskedMlp(4, 64, 64).forward(d["N"][:4], d["H"][:4], out[:4])

@@ -62,6 +62,11 @@ class Problem:
         self.dX.fill_(5.0)
         self.eng.matmul_backward(self.X, self.Y, self.dC, dX=self.dX)
         assert torch.equal(self.dX, first)
+        self.dX.fill_(5.0)          # at every element
+        self.eng.matmul_backward(self.X, self.Y, self.dC, dX=self.dX, all_x=True)
+        all_dx = self.G @ self.B.t()
+        assert bool(((self.dX.double().cpu() - all_dx).abs() <= (self.N + 1) * U * mags[0] + half * all_dx.abs() * (1 + 1e-3)).all())
+        assert torch.equal(self.dX.cpu()[self.a_on], first.cpu()[self.a_on])
         for whole, t in ((self.dXall, self.dX), (self.dYall, self.dY)):
             t.fill_(77.0)
             assert bool((whole == 77.0).all()), "outside"
