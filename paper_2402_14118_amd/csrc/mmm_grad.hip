@@ -16,6 +16,7 @@
 // way, one barrier per step.  In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that
 // eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "mmm_internal.h"
@@ -46,8 +47,51 @@ struct GradParams {
     const uint32_t *kinfo, *kmap;   // row-compacted mode; else null
     int64_t M, K, N, WA, WB;
     int32_t KBA, steps, bw_shift, accumulate;
+    int32_t splits, steps_per_split;
+    float *partials;     // splits > 1: [split][along L][along R, rows of whole quads]
     bool parts;          // the image is of floats in parts
 };
+
+// Four neighbouring results along R, from r on, of place l along L; `live`: the number of k there are.
+template <typename T, bool TO_X> __device__ __forceinline__ void store_results(const GradParams &p, uint32_t l, uint32_t r, uint32_t live, const floatx4 &v)
+{
+    if constexpr (TO_X) {
+        const uint64_t *const bits = p.a_bits != nullptr ? p.a_bits + (uint64_t)l * (uint64_t)p.WA : nullptr;   // null: all elements are wanted
+        T *const row = static_cast<T *>(p.out) + (int64_t)l * p.ldo;
+        if (p.kinfo == nullptr) {
+            const uint32_t on = bits != nullptr ? (uint32_t)(bits[r >> 6] >> (r & 63u)) : 0xfu;
+            typedef T vec __attribute__((ext_vector_type(4)));
+            typedef vec vec_any __attribute__((aligned(sizeof(T)), may_alias));
+            vec to;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) to[u] = on >> u & 1u ? (T)v[u] : (T)0.f;
+            if (r + 4 <= live) {
+                *reinterpret_cast<vec_any *>(row + r) = to;
+            } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (r + u < live) row[r + u] = to[u];
+            }
+        } else {   // (the row holds zeros)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (r + u >= live) continue;
+                const uint32_t k = p.kmap[r + u];
+                if (bits == nullptr || (bits[k >> 6] >> (k & 63u) & 1ull)) row[k] = (T)v[u];
+            }
+        }
+    } else {
+        const uint32_t k = p.kinfo != nullptr ? p.kmap[l] : l, jb = r >> p.bw_shift;
+        const bool on = p.b_bits[(uint64_t)k * (uint64_t)p.WB + (jb >> 6)] >> (jb & 63u) & 1ull;
+        typedef floatx4 vec_any __attribute__((aligned(4), may_alias));
+        vec_any *const dst = reinterpret_cast<vec_any *>(static_cast<float *>(p.out) + (int64_t)k * p.ldo + r);
+        if (p.accumulate) {
+            if (on) *dst = *dst + v;
+        } else {
+            *dst = on ? v : floatx4{0, 0, 0, 0};
+        }
+    }
+}
 
 template <typename T> __device__ __forceinline__ void multiply(const u32x4 &r, const u32x4 &l, floatx4 &acc)
 {
@@ -70,6 +114,7 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
     constexpr int STEP = ROWB / ESZ, PER = 16 / ESZ;          // elements of the contraction per step, and of a piece
     constexpr int NL = TL * 8 / NT, NR = TR * 8 / NT;         // pieces of 16 bytes per thread and step
     constexpr int TURNED_ROW = TR * ESZ, PIECES = TR / PER;   // dY: a row of dC in LDS, bytes and pieces
+    constexpr uint32_t TURN = TR / 16 < 8 ? TR / 16 - 1 : 7;  // and which of its sixteen columns take each other's place
     constexpr uint32_t OUTSIDE = 0x80000000u;                 // past the end of the buffers below, whatever else is added
     static_assert(NL * NT == TL * 8 && NR * NT == TR * 8, "whole pieces");
     __shared__ __align__(16) char lds[2][(TL + TR) * ROWB];
@@ -81,9 +126,10 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
     const uint32_t live = p.kinfo != nullptr ? *p.kinfo : (uint32_t)p.K;
     const uint32_t size_r = TO_X ? live : (uint32_t)p.N, size_l = TO_X ? (uint32_t)p.M : live;
     const uint32_t tiles_r = (size_r + TR - 1) / TR, tiles_l = (size_l + TL - 1) / TL, tiles = tiles_r * tiles_l;
-    if (blockIdx.x >= tiles) return;
-    const uint32_t q8 = tiles >> 3, rem = tiles & 7u, x = blockIdx.x & 7u;
-    const uint32_t t = x * q8 + min(x, rem) + (blockIdx.x >> 3);
+    const uint32_t all = tiles * (uint32_t)p.splits;
+    if (blockIdx.x >= all) return;
+    const uint32_t q8 = all >> 3, rem = all & 7u, x = blockIdx.x & 7u, id = x * q8 + min(x, rem) + (blockIdx.x >> 3);
+    const uint32_t split = id / tiles, t = id - split * tiles;
     const uint32_t panel = t / (8 * tiles_l), width = min(8u, tiles_r - panel * 8), in_panel = t - panel * 8 * tiles_l;
     const uint32_t r0 = (panel * 8 + in_panel % width) * TR, l0 = in_panel / width * TL;
 
@@ -199,7 +245,7 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
                 *reinterpret_cast<u32x4 *>(at + TL * ROWB + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = v;
             } else {
                 const uint32_t q = (uint32_t)tid + (uint32_t)n * NT, rho = q / PIECES, col = q % PIECES;   // col: piece of the row
-                const uint32_t turned = ESZ == 4 ? ((col >> 2) ^ (rho >> 2 & 7u)) << 2 | (col & 3u) : ((col >> 1) ^ (rho & 7u)) << 1 | (col & 1u);
+                const uint32_t turned = ESZ == 4 ? ((col >> 2) ^ (rho >> 2 & TURN)) << 2 | (col & 3u) : ((col >> 1) ^ (rho & TURN)) << 1 | (col & 1u);
                 *reinterpret_cast<u32x4 *>(at + TL * ROWB + rho * TURNED_ROW + (turned << 4)) = piece_r[n];
             }
         }
@@ -230,7 +276,7 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         const uint32_t rho = (uint32_t)((kk * 4 + s) * 4 + u);
-                        r[a][u] = *reinterpret_cast<const uint32_t *>(at + TL * ROWB + rho * TURNED_ROW + (((col0 >> 4) ^ (rho >> 2 & 7u)) << 6) + c * 4);
+                        r[a][u] = *reinterpret_cast<const uint32_t *>(at + TL * ROWB + rho * TURNED_ROW + (((col0 >> 4) ^ (rho >> 2 & TURN)) << 6) + c * 4);
                     }
                 } else {
                     // sixteen lanes read four rows of sixteen columns and get a column of four each
@@ -239,7 +285,7 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t rho = (uint32_t)((kk * 4 + s) * 8 + h * 4 + (c >> 2));
-                        const uint32_t where = TL * ROWB + rho * TURNED_ROW + (((col0 >> 4) ^ (rho & 7u)) << 5) + (uint32_t)(c & 3) * 8u;
+                        const uint32_t where = TL * ROWB + rho * TURNED_ROW + (((col0 >> 4) ^ (rho & TURN)) << 5) + (uint32_t)(c & 3) * 8u;
                         half[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)((lds_char *)lds[from] + where)));
                     }
                     r[a] = u32x4{half[0].x, half[0].y, half[1].x, half[1].y};
@@ -251,69 +297,54 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
                 for (int b = 0; b < FL; ++b) multiply<T>(r[a], l[b], acc[a][b]);
         }
     };
-    const int steps = p.steps;
-    fetch(0);
+    const int first = (int)split * p.steps_per_split, end = min(first + p.steps_per_split, p.steps);   // (no part is empty)
+    fetch(first);
     place(0);
-    for (int step = 0; step < steps; ++step) {
-        if (step + 1 < steps) fetch(step + 1);
+    for (int step = first, half = 0; step < end; ++step, half ^= 1) {
+        if (step + 1 < end) fetch(step + 1);
         __syncthreads();   // the step's operands are there; nobody reads the other half any more
-        compute(step & 1);
-        if (step + 1 < steps) place((step + 1) & 1);
+        compute(half);
+        if (step + 1 < end) place(half ^ 1);
     }
 
     // ---- results: a lane holds four neighbours along R of sixteen along L
+    const uint64_t pitch = (size_r + 3u) & ~3u;
+    float *const partials = p.splits > 1 ? p.partials + (uint64_t)split * size_l * pitch : nullptr;
 #pragma unroll
     for (int b = 0; b < FL; ++b) {
         const uint32_t l = l0 + (uint32_t)((wl * FL + b) * 16 + c);
         if (l >= size_l) continue;
-        if constexpr (TO_X) {
-            const uint64_t *const bits = p.a_bits != nullptr ? p.a_bits + (uint64_t)l * (uint64_t)p.WA : nullptr;   // null: all elements are wanted
-            T *const row = static_cast<T *>(p.out) + (int64_t)l * p.ldo;
 #pragma unroll
-            for (int a = 0; a < FR; ++a) {
-                const uint32_t k0 = r0 + (uint32_t)((wr * FR + a) * 16 + s * 4);
-                if (k0 >= live) continue;
-                if (p.kinfo == nullptr) {
-                    const uint32_t on = bits != nullptr ? (uint32_t)(bits[k0 >> 6] >> (k0 & 63u)) : 0xfu;
-                    typedef T vec __attribute__((ext_vector_type(4)));
-                    typedef vec vec_any __attribute__((aligned(sizeof(T)), may_alias));
-                    vec v;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) v[u] = on >> u & 1u ? (T)acc[a][b][u] : (T)0.f;
-                    if (k0 + 4 <= live) {
-                        *reinterpret_cast<vec_any *>(row + k0) = v;
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            if (k0 + u < live) row[k0 + u] = v[u];
-                    }
-                } else {   // (the row holds zeros)
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if (k0 + u >= live) continue;
-                        const uint32_t k = p.kmap[k0 + u];
-                        if (bits == nullptr || (bits[k >> 6] >> (k & 63u) & 1ull)) row[k] = (T)acc[a][b][u];
-                    }
-                }
-            }
-        } else {
-            const uint32_t k = p.kinfo != nullptr ? p.kmap[l] : l;
-            const uint64_t *const bits = p.b_bits + (uint64_t)k * (uint64_t)p.WB;
-            float *const row = static_cast<float *>(p.out) + (int64_t)k * p.ldo;
-#pragma unroll
-            for (int a = 0; a < FR; ++a) {
-                const uint32_t j = r0 + (uint32_t)((wr * FR + a) * 16 + s * 4), jb = j >> p.bw_shift;
-                if (j >= (uint32_t)p.N) continue;
-                const bool on = bits[jb >> 6] >> (jb & 63u) & 1ull;
-                typedef floatx4 vec_any __attribute__((aligned(4), may_alias));
-                vec_any *const dst = reinterpret_cast<vec_any *>(row + j);
-                if (p.accumulate) {
-                    if (on) *dst = *dst + acc[a][b];
-                } else {
-                    *dst = on ? acc[a][b] : floatx4{0, 0, 0, 0};
-                }
-            }
+        for (int a = 0; a < FR; ++a) {
+            const uint32_t r = r0 + (uint32_t)((wr * FR + a) * 16 + s * 4);
+            if (r >= size_r) continue;
+            if (partials != nullptr)
+                *reinterpret_cast<floatx4 *>(partials + l * pitch + r) = acc[a][b];
+            else
+                store_results<T, TO_X>(p, l, r, live, acc[a][b]);
         }
+    }
+}
+
+// The sums of a split contraction, in the order of its parts.
+template <typename T, bool TO_X> __global__ __launch_bounds__(256) void mmm_grad_join_kernel(const GradParams p)
+{
+    const uint32_t live = p.kinfo != nullptr ? *p.kinfo : (uint32_t)p.K;
+    const uint32_t size_r = TO_X ? live : (uint32_t)p.N, size_l = TO_X ? (uint32_t)p.M : live;
+    const uint64_t pitch = (size_r + 3u) & ~3u, total = (uint64_t)size_l * pitch;
+    const uint32_t r = (blockIdx.x * 256u + threadIdx.x) * 4u;
+    if (r >= size_r) return;
+    for (uint32_t l = blockIdx.y; l < size_l; l += gridDim.y) {
+        const float *const at = p.partials + l * pitch + r;
+        floatx4 sum = *reinterpret_cast<const floatx4 *>(at);
+        for (int32_t sp = 1; sp < p.splits; sp += 8) {
+            floatx4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = sp + i < p.splits ? *reinterpret_cast<const floatx4 *>(at + (uint64_t)(sp + i) * total) : floatx4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        store_results<T, TO_X>(p, l, r, live, sum);
     }
 }
 
@@ -341,13 +372,55 @@ hipError_t clear_rows(void *out, int64_t pitch, int64_t bytes, int64_t rows, con
     return hipGetLastError();
 }
 
-template <typename T, bool TO_X> hipError_t launch(const mmm_maps *m, const GradParams &p, hipStream_t s)
+// Tile and split of the contraction.  A tile of 128 x 128 feeds the matrix cores from LDS twice as well as one of 64 x 64, which leaves less of
+// small results idle and makes four times as many workgroups; where those are still few the contraction is split and the parts joined by a second launch.
+// Microseconds of a step of a workgroup where a compute unit has several (fitted, see estimate).
+struct GradPlan { int tile; int32_t splits, steps_per_split; };
+double estimate(int64_t size_r, int64_t size_l, int tile, int64_t steps, bool floats, int64_t splits)
 {
-    constexpr int WR = 2, WL = 2, FR = 4, FL = 4;
+    const double tiles = (double)((size_r + tile - 1) / tile) * (double)((size_l + tile - 1) / tile), per = (double)((steps + splits - 1) / splits);
+    const double step = floats ? (tile == 128 ? 2.0 : 0.6) : (tile == 128 ? 0.70 : 0.25);
+    const double alone = floats ? (tile == 128 ? 2.0 : 1.0) : (tile == 128 ? 1.0 : 0.7);   // of a workgroup that has a compute unit to itself
+    const double rounds = tiles * (double)splits / 256.0;
+    double us = per * (rounds <= 1.0 ? alone : std::max(alone, std::ceil(rounds) * step));
+    if (splits > 1) us += 3.0 + (double)splits * (double)size_r * (double)size_l * 8.0 / 3e6;
+    return us;
+}
+GradPlan plan_grad(int64_t size_r, int64_t size_l, int64_t steps, bool floats, size_t room, size_t bytes_per_split)
+{
+    GradPlan best{};
+    double least = -1.0;
+    for (int tile : {128, 64})
+        for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (want > 1 && ((size_t)want * bytes_per_split > room || steps < 4 * want)) break;
+            const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;   // no part is empty
+            const double us = estimate(size_r, size_l, tile, steps, floats, splits);
+            if (least < 0.0 || us < least) {
+                least = us;
+                best = {tile, (int32_t)splits, (int32_t)per};
+            }
+        }
+    return best;
+}
+
+template <typename T, bool TO_X> hipError_t launch(const mmm_maps *m, GradParams p, hipStream_t s)
+{
     const int64_t size_r = TO_X ? m->K : m->N, size_l = TO_X ? m->M : m->K;
-    const int64_t tiles = ((size_r + 16 * FR * WR - 1) / (16 * FR * WR)) * ((size_l + 16 * FL * WL - 1) / (16 * FL * WL));
-    if (tiles > (1LL << 32) / 1024 - 1) return hipErrorInvalidValue;   // threads of a launch
-    hipLaunchKernelGGL((mmm_grad_kernel<T, TO_X, WR, WL, FR, FL>), dim3((uint32_t)tiles), dim3(64 * WR * WL), 0, s, p);
+    // row-compacted mode: as many k as the most recent count has found (a guess: the kernels go by the number the device has)
+    const int64_t live = m->b_compact && m->stats_b_valid ? std::max<int64_t>(1, std::min<int64_t>(m->K, (int64_t)m->stats_rows_b)) : m->K;
+    const GradPlan plan = plan_grad(TO_X ? live : size_r, TO_X ? size_l : live, p.steps, sizeof(T) == 4, m->partial_bytes,
+                                    (size_t)((size_r + 3) & ~3LL) * (size_t)size_l * sizeof(float));
+    const int64_t tiles = ((size_r + plan.tile - 1) / plan.tile) * ((size_l + plan.tile - 1) / plan.tile) * plan.splits;
+    if (tiles > (1LL << 32) / 256 - 1) return hipErrorInvalidValue;   // threads of a launch
+    p.splits = plan.splits;
+    p.steps_per_split = plan.steps_per_split;
+    p.partials = m->partials;
+    void (*fn)(const GradParams) = plan.tile == 128 ? mmm_grad_kernel<T, TO_X, 2, 2, 4, 4> : mmm_grad_kernel<T, TO_X, 2, 2, 2, 2>;
+    hipLaunchKernelGGL(fn, dim3((uint32_t)tiles), dim3(256), 0, s, p);
+    if (plan.splits > 1) {
+        const dim3 grid((uint32_t)((size_r + 1023) / 1024), (uint32_t)std::min<int64_t>(size_l, 65535));
+        hipLaunchKernelGGL((mmm_grad_join_kernel<T, TO_X>), grid, dim3(256), 0, s, p);
+    }
     return hipGetLastError();
 }
 
