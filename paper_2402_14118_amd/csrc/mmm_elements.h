@@ -31,6 +31,20 @@ template <typename T> __device__ __forceinline__ void mmm_load_piece(const T *at
         for (int q = 0; q < MMM_PIECE; ++q) out[q] = q < n ? (float)at[q] : 0.f;
     }
 }
+// the same, left as they are
+template <typename T> struct mmm_raw_piece { typedef T type __attribute__((ext_vector_type(MMM_PIECE))); };
+template <typename T> __device__ __forceinline__ typename mmm_raw_piece<T>::type mmm_load_raw(const T *at, int n)
+{
+    typedef typename mmm_row_piece<T, MMM_PIECE>::type piece;
+    typename mmm_raw_piece<T>::type v;
+    if (n >= MMM_PIECE) {
+        v = *reinterpret_cast<const piece *>(at);
+    } else {
+#pragma unroll
+        for (int q = 0; q < MMM_PIECE; ++q) v[q] = q < n ? at[q] : (T)0.f;
+    }
+    return v;
+}
 // the first `n` of eight values to a row, rounded to nearest even once
 template <typename T> __device__ __forceinline__ void mmm_store_piece(T *at, int n, const float (&in)[MMM_PIECE])
 {

@@ -24,32 +24,92 @@ namespace {
 constexpr int PIECE = MMM_PIECE;
 constexpr int64_t MAX_GROUPS = 1 << 20;   // workgroups of a launch, which may have 2^32 threads: what is left over they take in turns
 
-template <int VALUES> __device__ __forceinline__ void add_over_lanes(float (&v)[VALUES])
+// The sum over the lanes of a wave, in lane 63: cross-lane moves of the vector unit, sixteen lanes first (a shuffle goes through LDS: 48 of them
+// per row were most of a row's time).
+template <int CTRL, int ROWS> __device__ __forceinline__ float lanes_below(float v)
 {
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2)
-#pragma unroll
-        for (int q = 0; q < VALUES; ++q) v[q] += __shfl_xor(v[q], step, 64);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, true));
+}
+__device__ __forceinline__ float add_over_lanes(float v)
+{
+    v += lanes_below<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8
+    v += lanes_below<0x112, 0xf>(v);
+    v += lanes_below<0x114, 0xf>(v);
+    v += lanes_below<0x118, 0xf>(v);
+    v += lanes_below<0x142, 0xa>(v);   // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+    v += lanes_below<0x143, 0xc>(v);
+    return v;
 }
 
-// Sums over a workgroup, the same in every lane.  `room`: VALUES floats per wave, not in use by a sum that waves may still be reading (two in turn).
-template <int VALUES> __device__ __forceinline__ void add_over_row(float (&v)[VALUES], float *room, int waves)
+// Sums over a workgroup of at most WAVES waves, the same in every lane.  `room`: not in use by a sum that waves may still be reading (two in turn), zero
+// behind the last wave's place.
+template <int VALUES, int WAVES> __device__ __forceinline__ void add_over_row(float (&v)[VALUES], float (*room)[WAVES])
 {
-    add_over_lanes(v);
-    if (waves == 1) return;
+    typedef float floatx4 __attribute__((ext_vector_type(4)));
+    static_assert(WAVES % 4 == 0, "");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (lane == 0)
 #pragma unroll
-        for (int q = 0; q < VALUES; ++q) room[wave * VALUES + q] = v[q];
+    for (int q = 0; q < VALUES; ++q) v[q] = add_over_lanes(v[q]);
+    if (lane == 63)
+#pragma unroll
+        for (int q = 0; q < VALUES; ++q) room[q][wave] = v[q];
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < VALUES; ++q) {
-        float sum = room[q];
-        for (int w = 1; w < waves; ++w) sum += room[w * VALUES + q];
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; w += 4) {
+            const floatx4 four = *reinterpret_cast<const floatx4 *>(&room[q][w]);
+            sum += (four.x + four.y) + (four.z + four.w);
+        }
         v[q] = sum;
     }
 }
+template <int N> __device__ __forceinline__ void clear_rooms(float *rooms)
+{
+    for (int q = threadIdx.x; q < N; q += blockDim.x) rooms[q] = 0.f;
+    __syncthreads();
+}
 
+// The pieces of a row that this lane has: V of them, a workgroup's width apart.  WHOLE: rows of eight elements and more, all loads are whole pieces
+// that exist, without a branch around any (with branches each load was waited for where it stood, and everything under way with it: a
+// row's gradients took four times as long): a piece that ends behind the row begins earlier, at the row's last eight elements, and
+// what of it is another lane's counts for nothing here.  Else (a row is one short piece) element by element.
+template <bool WHOLE, int V> struct Pieces {
+    int at[V], first[V], count[V];   // where piece i is read; its elements that are this lane's: first, and how many
+    __device__ __forceinline__ explicit Pieces(int N)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int col = (i * (int)blockDim.x + (int)threadIdx.x) * PIECE;
+            at[i] = WHOLE ? min(col, N - PIECE) : 0;
+            first[i] = WHOLE ? min(col - at[i], PIECE) : 0;
+            count[i] = WHOLE ? PIECE - first[i] : threadIdx.x == 0 ? N : 0;
+        }
+    }
+    __device__ __forceinline__ bool mine(int i, int q) const { return WHOLE ? q >= first[i] : q < count[i]; }
+    template <typename T> __device__ __forceinline__ typename mmm_raw_piece<T>::type load(const T *row, int i) const
+    {
+        if constexpr (WHOLE) {
+            typedef typename mmm_row_piece<T, PIECE>::type piece;
+            return *reinterpret_cast<const piece *>(row + at[i]);
+        } else {
+            return mmm_load_raw(row, count[i]);
+        }
+    }
+    template <typename T> __device__ __forceinline__ void store(T *row, int i, const float (&v)[PIECE]) const
+    {
+        if (WHOLE && first[i] == 0) {
+            mmm_store_piece(row + at[i], PIECE, v);
+        } else {
+#pragma unroll
+            for (int q = 0; q < PIECE; ++q)
+                if (mine(i, q)) row[at[i] + q] = (T)v[q];
+        }
+    }
+};
+
+// Operands that are not there are given an address that may be read all the same, and a flag: what is read there is replaced.
 struct NormParams {
     mmm_block_norm_desc d;
     float inv_n;
@@ -57,82 +117,92 @@ struct NormParams {
     int64_t ldh, ldy, ldgate;
     void *h_out, *n;
     int64_t ldh_out, ldn;
+    const void *row_gates;   // MMM_GATE_ROW: the values
+    bool has_y, has_gate, has_post_weight, has_post_bias, has_pre_weight, has_pre_bias;   // has_gate: a value per column or element
 };
 
-// the pieces of a row that this lane has: V of them, a workgroup's width apart
-#define MMM_FOR_PIECES(p, col, left)                                                                              \
-    _Pragma("unroll") for (int p = 0; p < V; ++p)                                                                 \
-        if (const int col = (p * (int)blockDim.x + (int)threadIdx.x) * PIECE, left = N - col; left > 0)
-
-template <typename T, typename TH, typename TY, int V> __global__ __launch_bounds__(1024) void mmm_block_norm_kernel(const NormParams p)
+// values of a piece, or one and the same where there are none
+template <typename R> __device__ __forceinline__ void values_or(const R &raw, bool there, float otherwise, float (&out)[PIECE])
 {
-    __shared__ float rooms[2][4][16];   // (rows in turn: of a row, a wave may still read what another has gone past)
-    const int N = (int)p.d.N, waves = (int)blockDim.x >> 6;
+#pragma unroll
+    for (int q = 0; q < PIECE; ++q) out[q] = there ? (float)raw[q] : otherwise;
+}
+
+template <typename T, typename TH, typename TY, int V, int WAVES, bool WHOLE> __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_kernel(const NormParams p)
+{
+    __shared__ __align__(16) float rooms[2][4][1][WAVES];   // (rows in turn: of a row, a wave may still read what another has gone past)
+    clear_rooms<2 * 4 * WAVES>(&rooms[0][0][0][0]);
+    const Pieces<WHOLE, V> mine((int)p.d.N);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < p.d.M; row += gridDim.x, turn ^= 1) {
         float h[V][PIECE], v[V][PIECE];
-        MMM_FOR_PIECES(i, col, left) mmm_load_piece(static_cast<const TH *>(p.h) + row * p.ldh + col, left, h[i]);
+        typename mmm_raw_piece<TH>::type raw_h[V];
+        typename mmm_raw_piece<TY>::type raw_y[V];
+        typename mmm_raw_piece<T>::type raw_gate[V], raw_w[V], raw_b[V], raw_w2[V], raw_b2[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            raw_h[i] = mine.load(static_cast<const TH *>(p.h) + row * p.ldh, i);
+            raw_y[i] = mine.load(static_cast<const TY *>(p.y) + row * p.ldy, i);
+            raw_gate[i] = mine.load(static_cast<const T *>(p.gate) + row * p.ldgate, i);
+            raw_w[i] = mine.load(static_cast<const T *>(p.post_weight), i);
+            raw_b[i] = mine.load(static_cast<const T *>(p.post_bias), i);
+            raw_w2[i] = mine.load(static_cast<const T *>(p.pre_weight), i);
+            raw_b2[i] = mine.load(static_cast<const T *>(p.pre_bias), i);
+        }
         // 1 / the deviation of the row in x, whose mean is taken off it; `of`: which of the two norms
         auto standard = [&](float (&x)[V][PIECE], int32_t kind, int of) __attribute__((always_inline)) -> float {
             float sum[1] = {0.f};
             if (kind == MMM_NORM_LAYER) {
-                MMM_FOR_PIECES(i, col, left)
-                {
 #pragma unroll
-                    for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q];   // (elements past the row are zero)
-                }
-                add_over_row(sum, rooms[turn][of], waves);
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q];   // (elements that are not this lane's are zero)
+                add_over_row(sum, rooms[turn][of]);
                 const float mean = sum[0] * p.inv_n;
-                MMM_FOR_PIECES(i, col, left)
-                {
 #pragma unroll
-                    for (int q = 0; q < PIECE; ++q) x[i][q] = q < left ? x[i][q] - mean : 0.f;
-                }
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int q = 0; q < PIECE; ++q) x[i][q] = mine.mine(i, q) ? x[i][q] - mean : 0.f;
                 sum[0] = 0.f;
             }
-            MMM_FOR_PIECES(i, col, left)
-            {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q] * x[i][q];
-            }
-            add_over_row(sum, rooms[turn][2 + of], waves);
+            add_over_row(sum, rooms[turn][2 + of]);
             return 1.f / sqrtf(sum[0] * p.inv_n + p.d.eps);
         };
-        auto affine = [&](float (&x)[PIECE], float r, const void *weight, const void *bias, int col, int left) __attribute__((always_inline)) {
-            float w[PIECE], b[PIECE];
-            if (weight != nullptr) mmm_load_piece(static_cast<const T *>(weight) + col, left, w);
-            if (bias != nullptr) mmm_load_piece(static_cast<const T *>(bias) + col, left, b);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) {
-                x[q] *= r;
-                if (weight != nullptr) x[q] *= w[q];
-                if (bias != nullptr) x[q] += b[q];
+                h[i][q] = mine.mine(i, q) ? (float)raw_h[i][q] : 0.f;
+                v[i][q] = mine.mine(i, q) ? (float)raw_y[i][q] : 0.f;
             }
-        };
-        if (p.y != nullptr) {
-            MMM_FOR_PIECES(i, col, left) mmm_load_piece(static_cast<const TY *>(p.y) + row * p.ldy + col, left, v[i]);
+        if (p.has_y) {
             const float r = p.d.post != MMM_NORM_NONE ? standard(v, p.d.post, 0) : 1.f;
-            const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(p.gate)[row] : 1.f;
-            MMM_FOR_PIECES(i, col, left)
-            {
-                affine(v[i], r, p.post_weight, p.post_bias, col, left);
-                float g[PIECE];
-                if (p.d.gate >= MMM_GATE_COL)
-                    mmm_load_piece(static_cast<const T *>(p.gate) + (p.d.gate == MMM_GATE_FULL ? row * p.ldgate : 0) + col, left, g);
+            const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(p.row_gates)[row] : 1.f;
 #pragma unroll
-                for (int q = 0; q < PIECE; ++q) {
-                    h[i][q] = p.d.alpha * h[i][q] + (p.d.gate >= MMM_GATE_COL ? g[q] : row_gate) * v[i][q];
-                    if (q >= left) h[i][q] = 0.f;
-                }
-                if (p.h_out != nullptr) mmm_store_piece(static_cast<TH *>(p.h_out) + row * p.ldh_out + col, left, h[i]);
+            for (int i = 0; i < V; ++i) {
+                float w[PIECE], b[PIECE], g[PIECE];
+                values_or(raw_w[i], p.has_post_weight, 1.f, w);
+                values_or(raw_b[i], p.has_post_bias, 0.f, b);
+                values_or(raw_gate[i], p.has_gate, row_gate, g);
+#pragma unroll
+                for (int q = 0; q < PIECE; ++q) h[i][q] = mine.mine(i, q) ? p.d.alpha * h[i][q] + g[q] * (v[i][q] * r * w[q] + b[q]) : 0.f;
+                if (p.h_out != nullptr) mine.store(static_cast<TH *>(p.h_out) + row * p.ldh_out, i, h[i]);
             }
         }
         if (p.d.pre != MMM_NORM_NONE) {
             const float r = standard(h, p.d.pre, 1);
-            MMM_FOR_PIECES(i, col, left)
-            {
-                affine(h[i], r, p.pre_weight, p.pre_bias, col, left);
-                mmm_store_piece(static_cast<T *>(p.n) + row * p.ldn + col, left, h[i]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float w[PIECE], b[PIECE];
+                values_or(raw_w2[i], p.has_pre_weight, 1.f, w);
+                values_or(raw_b2[i], p.has_pre_bias, 0.f, b);
+#pragma unroll
+                for (int q = 0; q < PIECE; ++q) h[i][q] = h[i][q] * r * w[q] + b[q];
+                mine.store(static_cast<T *>(p.n) + row * p.ldn, i, h[i]);
             }
         }
     }
@@ -143,19 +213,56 @@ enum { SUM_PRE_WEIGHT, SUM_PRE_BIAS, SUM_POST_WEIGHT, SUM_POST_BIAS, SUM_GATE, S
 
 struct NormGradParams {
     mmm_block_norm_desc d;
-    mmm_block_norm_grads g;
+    mmm_block_norm_grads g;   // (operands that are not there: as above)
     float inv_n;
     float *partials;        // [workgroup][sum asked for][N]
     int32_t place[SUMS];    // of a sum among those asked for; -1: not asked for
     int32_t sums;
+    const void *row_gates;
+    bool has_d_h_out, has_gate, has_post_weight, has_post_bias, has_pre_weight, block;
 };
 
-template <typename T, typename TH, typename TY, int V> __global__ __launch_bounds__(1024) void mmm_block_norm_grad_kernel(const NormGradParams p)
+// What a row takes from memory: asked for while the row before is worked on.
+template <typename T, typename TH, typename TY, int V, bool WHOLE> struct GradRow {
+    typename mmm_raw_piece<TH>::type x[V], d[V];
+    typename mmm_raw_piece<T>::type dn[V], gate[V];
+    typename mmm_raw_piece<TY>::type y[V];
+    __device__ __forceinline__ void load(const NormGradParams &p, const Pieces<WHOLE, V> &mine, int64_t row)
+    {
+        const mmm_block_norm_grads &g = p.g;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            x[i] = mine.load(static_cast<const TH *>(g.h_out) + row * g.ldh_out, i);
+            dn[i] = mine.load(static_cast<const T *>(g.d_n) + row * g.ldd_n, i);
+            d[i] = mine.load(static_cast<const TH *>(g.d_h_out) + row * g.ldd_h_out, i);
+            y[i] = mine.load(static_cast<const TY *>(g.y) + row * g.ldy, i);
+            gate[i] = mine.load(static_cast<const T *>(g.gate_values) + row * g.ldgate, i);
+        }
+    }
+};
+// What all rows share.
+template <typename T, int V, bool WHOLE> struct GradColumns {
+    typename mmm_raw_piece<T>::type pre_weight[V], post_weight[V], post_bias[V];
+    __device__ __forceinline__ void load(const NormGradParams &p, const Pieces<WHOLE, V> &mine, bool biases)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            pre_weight[i] = mine.load(static_cast<const T *>(p.g.pre_weight), i);
+            post_weight[i] = mine.load(static_cast<const T *>(p.g.post_weight), i);
+            post_bias[i] = biases ? mine.load(static_cast<const T *>(p.g.post_bias), i) : post_weight[i];
+        }
+    }
+};
+
+// BIASES: the norm behind the block has a bias, or sums for biases are asked for
+template <typename T, typename TH, typename TY, int V, int WAVES, bool BIASES, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const NormGradParams p)
 {
-    __shared__ float rooms[2][4][48];   // (rows in turn, as above)
+    __shared__ __align__(16) float rooms[2][4][3][WAVES];   // (rows in turn, as above)
+    clear_rooms<2 * 4 * 3 * WAVES>(&rooms[0][0][0][0]);
     const mmm_block_norm_grads &g = p.g;
-    const int N = (int)p.d.N, waves = (int)blockDim.x >> 6;
-    const bool pre = p.d.pre != MMM_NORM_NONE, block = g.y != nullptr, post = p.d.post != MMM_NORM_NONE;
+    const Pieces<WHOLE, V> mine((int)p.d.N);
+    const bool pre = p.d.pre != MMM_NORM_NONE, block = p.block, post = p.d.post != MMM_NORM_NONE;
     const bool pre_mean = p.d.pre == MMM_NORM_LAYER, post_mean = p.d.post == MMM_NORM_LAYER;
     float sums[SUMS][V][PIECE];
 #pragma unroll
@@ -165,132 +272,125 @@ template <typename T, typename TH, typename TY, int V> __global__ __launch_bound
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) sums[s][i][q] = 0.f;
 
+    GradColumns<T, V, WHOLE> columns;
+    if (V == 1) columns.load(p, mine, BIASES);   // (wider rows have no registers for them)
+    GradRow<T, TH, TY, V, WHOLE> next;
+    next.load(p, mine, blockIdx.x);   // (there are no more workgroups than rows)
     int turn = 0;
     for (int64_t row = blockIdx.x; row < p.d.M; row += gridDim.x, turn ^= 1) {
-        float x[V][PIECE], dn[V][PIECE], d[V][PIECE], y[V][PIECE];
-        MMM_FOR_PIECES(i, col, left)
-        {
-            if (pre) {
-                mmm_load_piece(static_cast<const TH *>(g.h_out) + row * g.ldh_out + col, left, x[i]);
-                mmm_load_piece(static_cast<const T *>(g.d_n) + row * g.ldd_n + col, left, dn[i]);
-            }
-            if (g.d_h_out != nullptr)
-                mmm_load_piece(static_cast<const TH *>(g.d_h_out) + row * g.ldd_h_out + col, left, d[i]);
-            else
+        float x[V][PIECE], dn[V][PIECE], d[V][PIECE], y[V][PIECE], gate[V][PIECE];
+        const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(p.row_gates)[row] : 1.f;
 #pragma unroll
-                for (int q = 0; q < PIECE; ++q) d[i][q] = 0.f;
-            if (block) mmm_load_piece(static_cast<const TY *>(g.y) + row * g.ldy + col, left, y[i]);
+        for (int i = 0; i < V; ++i) {
+            values_or(next.gate[i], p.has_gate, row_gate, gate[i]);
+#pragma unroll
+            for (int q = 0; q < PIECE; ++q) {   // zeros for what is not there, and what is another lane's
+                const bool on = mine.mine(i, q);
+                x[i][q] = pre && on ? (float)next.x[i][q] : 0.f;
+                dn[i][q] = pre && on ? (float)next.dn[i][q] : 0.f;
+                d[i][q] = p.has_d_h_out && on ? (float)next.d[i][q] : 0.f;
+                y[i][q] = block && on ? (float)next.y[i][q] : 0.f;
+            }
         }
+        if (V > 1) columns.load(p, mine, BIASES);
+        next.load(p, mine, min(row + (int64_t)gridDim.x, p.d.M - 1));
         // both rows standardised together: one sum for means, one for variances
         float s2[2] = {0.f, 0.f};
         if (pre_mean || post_mean) {
-            MMM_FOR_PIECES(i, col, left)
-            {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) {
-                    if (pre_mean) s2[0] += x[i][q];
-                    if (post_mean) s2[1] += y[i][q];
+                    s2[0] += x[i][q];
+                    s2[1] += y[i][q];
                 }
-            }
-            add_over_row(s2, rooms[turn][0], waves);
+            add_over_row(s2, rooms[turn][0]);
             const float mx = pre_mean ? s2[0] * p.inv_n : 0.f, my = post_mean ? s2[1] * p.inv_n : 0.f;
-            MMM_FOR_PIECES(i, col, left)
-            {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) {
-                    if (pre_mean) x[i][q] = q < left ? x[i][q] - mx : 0.f;
-                    if (post_mean) y[i][q] = q < left ? y[i][q] - my : 0.f;
+                    x[i][q] = mine.mine(i, q) ? x[i][q] - mx : 0.f;
+                    y[i][q] = mine.mine(i, q) ? y[i][q] - my : 0.f;
                 }
-            }
             s2[0] = s2[1] = 0.f;
         }
-        MMM_FOR_PIECES(i, col, left)
-        {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) {
-                if (pre) s2[0] += x[i][q] * x[i][q];
-                if (post) s2[1] += y[i][q] * y[i][q];
+                s2[0] += x[i][q] * x[i][q];
+                s2[1] += y[i][q] * y[i][q];
             }
-        }
-        if (pre || post) add_over_row(s2, rooms[turn][1], waves);
-        const float rx = 1.f / sqrtf(s2[0] * p.inv_n + p.d.eps), ry = 1.f / sqrtf(s2[1] * p.inv_n + p.d.eps);
+        add_over_row(s2, rooms[turn][1]);
+        const float rx = 1.f / sqrtf(s2[0] * p.inv_n + p.d.eps), ry = post ? 1.f / sqrtf(s2[1] * p.inv_n + p.d.eps) : 1.f;
         // through the norm in front of the next block: d becomes the gradient of h'
         if (pre) {
             float c[2] = {0.f, 0.f};
-            MMM_FOR_PIECES(i, col, left)
-            {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
                 float w[PIECE];
-                if (g.pre_weight != nullptr) mmm_load_piece(static_cast<const T *>(g.pre_weight) + col, left, w);
+                values_or(columns.pre_weight[i], p.has_pre_weight, 1.f, w);
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) {
                     x[i][q] *= rx;
-                    if (p.place[SUM_PRE_WEIGHT] >= 0) sums[SUM_PRE_WEIGHT][i][q] += dn[i][q] * x[i][q];
-                    if (p.place[SUM_PRE_BIAS] >= 0) sums[SUM_PRE_BIAS][i][q] += dn[i][q];
-                    if (g.pre_weight != nullptr) dn[i][q] *= w[q];
+                    sums[SUM_PRE_WEIGHT][i][q] += dn[i][q] * x[i][q];
+                    if (BIASES) sums[SUM_PRE_BIAS][i][q] += dn[i][q];
+                    dn[i][q] *= w[q];
                     c[0] += dn[i][q] * x[i][q];
                     c[1] += dn[i][q];
                 }
             }
-            add_over_row(c, rooms[turn][2], waves);
+            add_over_row(c, rooms[turn][2]);
             const float along = c[0] * p.inv_n, mean = pre_mean ? c[1] * p.inv_n : 0.f;
-            MMM_FOR_PIECES(i, col, left)
-            {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) d[i][q] += rx * (dn[i][q] - x[i][q] * along - mean);
-            }
         }
         if (g.d_h != nullptr) {
             const float alpha = block ? p.d.alpha : 1.f;
-            MMM_FOR_PIECES(i, col, left)
-            {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
                 float out[PIECE];
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) out[q] = alpha * d[i][q];
-                mmm_store_piece(static_cast<TH *>(g.d_h) + row * g.ldd_h + col, left, out);
+                mine.store(static_cast<TH *>(g.d_h) + row * g.ldd_h, i, out);
             }
         }
         if (!block) continue;   // (uniform: no sum is under way)
         // through gate and norm behind the block: d becomes the gradient of y
-        const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(g.gate_values)[row] : 1.f;
         float c[3] = {0.f, 0.f, 0.f};
-        MMM_FOR_PIECES(i, col, left)
-        {
-            float gate[PIECE], w[PIECE], b[PIECE], dgate[PIECE];
-            if (p.d.gate >= MMM_GATE_COL)
-                mmm_load_piece(static_cast<const T *>(g.gate_values) + (p.d.gate == MMM_GATE_FULL ? row * g.ldgate : 0) + col, left, gate);
-            if (g.post_weight != nullptr) mmm_load_piece(static_cast<const T *>(g.post_weight) + col, left, w);
-            if (g.post_bias != nullptr) mmm_load_piece(static_cast<const T *>(g.post_bias) + col, left, b);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float w[PIECE], b[PIECE], dgate[PIECE];
+            values_or(columns.post_weight[i], p.has_post_weight, 1.f, w);
+            values_or(columns.post_bias[i], BIASES && p.has_post_bias, 0.f, b);
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) {
-                if (q >= left) d[i][q] = 0.f;   // (past the row; the mean has been taken off there, too)
-                if (post) y[i][q] *= ry;
-                float v = y[i][q];
-                if (g.post_weight != nullptr) v *= w[q];
-                if (g.post_bias != nullptr) v += b[q];
-                dgate[q] = d[i][q] * v;
+                if (!mine.mine(i, q)) d[i][q] = 0.f;   // (the mean has been taken off there, too)
+                y[i][q] *= ry;
+                dgate[q] = d[i][q] * (y[i][q] * w[q] + b[q]);
                 c[2] += dgate[q];
-                if (p.place[SUM_GATE] >= 0) sums[SUM_GATE][i][q] += dgate[q];
-                d[i][q] *= p.d.gate >= MMM_GATE_COL ? gate[q] : row_gate;
-                if (p.place[SUM_POST_WEIGHT] >= 0) sums[SUM_POST_WEIGHT][i][q] += d[i][q] * y[i][q];
-                if (p.place[SUM_POST_BIAS] >= 0) sums[SUM_POST_BIAS][i][q] += d[i][q];
-                if (g.post_weight != nullptr) d[i][q] *= w[q];
+                sums[SUM_GATE][i][q] += dgate[q];
+                d[i][q] *= gate[i][q];
+                sums[SUM_POST_WEIGHT][i][q] += d[i][q] * y[i][q];
+                if (BIASES) sums[SUM_POST_BIAS][i][q] += d[i][q];
+                d[i][q] *= w[q];
                 c[0] += d[i][q] * y[i][q];
                 c[1] += d[i][q];
             }
-            if (p.d.gate == MMM_GATE_FULL && g.d_gate != nullptr)
-                mmm_store_piece(static_cast<T *>(g.d_gate) + row * g.ldd_gate + col, left, dgate);
+            if (p.d.gate == MMM_GATE_FULL && g.d_gate != nullptr) mine.store(static_cast<T *>(g.d_gate) + row * g.ldd_gate, i, dgate);
         }
-        const bool row_sum = p.d.gate == MMM_GATE_ROW && g.d_gate != nullptr;
-        if (post || row_sum) add_over_row(c, rooms[turn][3], waves);
-        if (row_sum && threadIdx.x == 0) static_cast<float *>(g.d_gate)[row] = c[2];
+        add_over_row(c, rooms[turn][3]);
+        if (p.d.gate == MMM_GATE_ROW && g.d_gate != nullptr && threadIdx.x == 0) static_cast<float *>(g.d_gate)[row] = c[2];
         if (g.d_y != nullptr) {
-            const float along = c[0] * p.inv_n, mean = post_mean ? c[1] * p.inv_n : 0.f;
-            MMM_FOR_PIECES(i, col, left)
-            {
-                if (post)
+            const float along = post ? c[0] * p.inv_n : 0.f, mean = post_mean ? c[1] * p.inv_n : 0.f;
 #pragma unroll
-                    for (int q = 0; q < PIECE; ++q) d[i][q] = ry * (d[i][q] - y[i][q] * along - mean);
-                mmm_store_piece(static_cast<TY *>(g.d_y) + row * g.ldd_y + col, left, d[i]);
+            for (int i = 0; i < V; ++i) {
+#pragma unroll
+                for (int q = 0; q < PIECE; ++q) d[i][q] = ry * (d[i][q] - y[i][q] * along - mean);
+                mine.store(static_cast<TY *>(g.d_y) + row * g.ldd_y, i, d[i]);
             }
         }
     }
@@ -298,7 +398,8 @@ template <typename T, typename TH, typename TY, int V> __global__ __launch_bound
 #pragma unroll
     for (int s = 0; s < SUMS; ++s) {
         if (p.place[s] < 0) continue;
-        MMM_FOR_PIECES(i, col, left) mmm_store_piece(p.partials + ((int64_t)blockIdx.x * p.sums + p.place[s]) * N + col, left, sums[s][i]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) mine.store(p.partials + ((int64_t)blockIdx.x * p.sums + p.place[s]) * p.d.N, i, sums[s][i]);
     }
 }
 
@@ -347,7 +448,7 @@ template <typename T, typename TC> __global__ __launch_bounds__(64 * ACT_WAVES) 
     }
 }
 
-// Partial sums added in order: out[s][j] = sum over g of partials[g][s][j].  Sixteen waves take every sixteenth g each.
+// Partial sums added in order: out[s][j] = sum over g of partials[g][s][j].  A wave takes every sixteenth g of 64 columns, eight of them in flight.
 struct ReduceParams {
     const float *partials;
     int64_t groups, N;
@@ -366,13 +467,19 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void mmm_add_partials_kernel(con
     for (int q = 1; q < SUMS; ++q)
         if (q == s) out = p.out[q];
     for (int64_t col0 = (int64_t)blockIdx.x * 64; col0 < p.N; col0 += (int64_t)gridDim.x * 64) {
-        const int64_t col = col0 + lane;
+        const int64_t col = min(col0 + lane, p.N - 1), step = (int64_t)p.sums * p.N;
+        const float *const at = p.partials + (int64_t)s * p.N + col;
         float sum = 0.f;
-        if (col < p.N)
-            for (int64_t g = wave; g < p.groups; g += REDUCE_WAVES) sum += p.partials[(g * p.sums + s) * p.N + col];
+        for (int64_t g = wave; g < p.groups; g += 8 * REDUCE_WAVES) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = at[min(g + i * REDUCE_WAVES, p.groups - 1) * step];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += g + i * REDUCE_WAVES < p.groups ? v[i] : 0.f;
+        }
         room[wave][lane] = sum;
         __syncthreads();
-        if (wave == 0 && col < p.N) {
+        if (wave == 0 && col0 + lane < p.N) {
             for (int w = 1; w < REDUCE_WAVES; ++w) sum += room[w][lane];
             out[col] = sum;
         }
@@ -386,14 +493,13 @@ hipError_t add_partials(const ReduceParams &r, hipStream_t s)
     return hipGetLastError();
 }
 
-// Threads and pieces per lane for a row: one piece as long as a workgroup has room.
+// Threads and pieces per lane for a row: one piece as long as the workgroup has room.
 struct RowShape { uint32_t threads; int pieces; };
-RowShape row_shape(int64_t N, uint32_t most)
+RowShape row_shape(int64_t N)
 {
     const uint32_t lanes = (uint32_t)((N + PIECE - 1) / PIECE);
-    const int pieces = lanes <= most ? 1 : lanes <= 2 * most ? 2 : 4;
-    const uint32_t threads = ((lanes + (uint32_t)pieces - 1) / (uint32_t)pieces + 63) / 64 * 64;
-    return {threads, pieces};
+    const int pieces = lanes <= 512 ? 1 : lanes <= 1024 ? 2 : 4;
+    return {((lanes + (uint32_t)pieces - 1) / (uint32_t)pieces + 63) / 64 * 64, pieces};
 }
 
 // calls f with the types of a case
@@ -413,7 +519,13 @@ template <typename F> auto with_types(const mmm_block_norm_desc &d, F f)
     return with_stream_types<float>(d, f);
 }
 
-int64_t norm_grad_groups(int64_t M) { return std::min<int64_t>(M, 512); }
+// Workgroups of the gradients: as many as the registers of the chip hold at a time (8 waves on a compute unit), so that partial sums are few, and
+// all with the same number of rows but for one.  2048 x 4096 bf16: 256 groups 28.6 us and 4.0 for adding up, 512 32.3 and 5.5, 1024 38.8 and 8.3.
+int64_t norm_grad_groups(int64_t M, int64_t N)
+{
+    const int64_t slots = 256 * std::max<int64_t>(1, 512 / row_shape(N).threads), rows = (M + slots - 1) / slots;
+    return (M + rows - 1) / rows;
+}
 int64_t act_strips(int64_t N) { return (N + ACT_COLS - 1) / ACT_COLS; }
 int64_t act_shares(int64_t M, int64_t N)
 {
@@ -426,32 +538,65 @@ hipError_t mmm_launch_block_norm(const mmm_block_norm_desc &d, const void *h, in
                                  const void *post_weight, const void *post_bias, const void *pre_weight, const void *pre_bias, void *h_out,
                                  int64_t ldh_out, void *n, int64_t ldn, hipStream_t s)
 {
-    const RowShape shape = row_shape(d.N, 1024);
     if (d.M < 1 || d.N < 1 || d.N > MMM_NORM_MAX_WIDTH) return hipErrorInvalidValue;
-    const NormParams p{d, 1.f / (float)d.N, h, y, gate, post_weight, post_bias, pre_weight, pre_bias, ldh, ldy, ldgate, h_out, n, ldh_out, ldn};
+    const RowShape shape = row_shape(d.N);
+    NormParams p{d, 1.f / (float)d.N, h, y, gate, post_weight, post_bias, pre_weight, pre_bias, ldh, ldy, ldgate, h_out, n, ldh_out, ldn,
+                 gate, y != nullptr, d.gate >= MMM_GATE_COL, post_weight != nullptr, post_bias != nullptr, pre_weight != nullptr, pre_bias != nullptr};
+    // what is not there is read from h, whose rows are N elements of no smaller a type (without a block y has that type, too)
+    if (y == nullptr) {
+        p.y = h;
+        p.ldy = ldh;
+        p.d.dt_y = d.dt_h;
+    }
+    if (d.gate < MMM_GATE_FULL) p.ldgate = 0;
+    if (!p.has_gate) p.gate = h;
+    for (const void **q : {&p.post_weight, &p.post_bias, &p.pre_weight, &p.pre_bias})
+        if (*q == nullptr) *q = h;
     (void)hipGetLastError();
-    with_types(d, [&](auto t, auto th, auto ty) {
+    with_types(p.d, [&](auto t, auto th, auto ty) {
         typedef decltype(t) T;
         typedef decltype(th) TH;
         typedef decltype(ty) TY;
-        void (*fn)(const NormParams) = shape.pieces == 1   ? mmm_block_norm_kernel<T, TH, TY, 1>
-                                       : shape.pieces == 2 ? mmm_block_norm_kernel<T, TH, TY, 2>
-                                                           : mmm_block_norm_kernel<T, TH, TY, 4>;
+        void (*fn)(const NormParams) = d.N < PIECE         ? mmm_block_norm_kernel<T, TH, TY, 1, 4, false>
+                                       : shape.pieces == 1 ? shape.threads <= 256 ? mmm_block_norm_kernel<T, TH, TY, 1, 4, true> : mmm_block_norm_kernel<T, TH, TY, 1, 8, true>
+                                       : shape.pieces == 2 ? mmm_block_norm_kernel<T, TH, TY, 2, 8, true>
+                                                           : mmm_block_norm_kernel<T, TH, TY, 4, 16, true>;
         hipLaunchKernelGGL(fn, dim3((uint32_t)std::min(d.M, MAX_GROUPS)), dim3(shape.threads), 0, s, p);
         return 0;
     });
     return hipGetLastError();
 }
 
-size_t mmm_block_norm_grad_bytes(int64_t M, int64_t N) { return (size_t)norm_grad_groups(M) * (size_t)N * SUMS * sizeof(float); }
+size_t mmm_block_norm_grad_bytes(int64_t M, int64_t N) { return (size_t)norm_grad_groups(M, N) * (size_t)N * SUMS * sizeof(float); }
 
 hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_block_norm_grads &g, void *workspace, hipStream_t s)
 {
-    const RowShape shape = row_shape(d.N, 1024);
     if (d.M < 1 || d.N < 1 || d.N > MMM_NORM_MAX_WIDTH) return hipErrorInvalidValue;
-    NormGradParams p{d, g, 1.f / (float)d.N, static_cast<float *>(workspace), {}, 0};
+    const RowShape shape = row_shape(d.N);
+    NormGradParams p{d, g, 1.f / (float)d.N, static_cast<float *>(workspace), {}, 0, g.gate_values, g.d_h_out != nullptr, d.gate >= MMM_GATE_COL, g.post_weight != nullptr,
+                     g.post_bias != nullptr, g.pre_weight != nullptr, g.y != nullptr};
+    // What is not there is read from what is: h' and d_n with a norm in front, else d_h' and y (the types of a block that is not there are
+    // those of h, and the rows of a narrower type end sooner).
+    const bool pre = d.pre != MMM_NORM_NONE;
+    if (!pre) {
+        p.g.h_out = p.g.d_n = g.d_h_out;
+        p.g.ldh_out = p.g.ldd_n = g.ldd_h_out;
+    }
+    if (g.d_h_out == nullptr) {
+        p.g.d_h_out = g.h_out;
+        p.g.ldd_h_out = g.ldh_out;
+    }
+    if (g.y == nullptr) {
+        p.g.y = p.g.h_out;
+        p.g.ldy = p.g.ldh_out;
+        p.d.dt_y = d.dt_h;
+    }
+    if (d.gate < MMM_GATE_FULL) p.g.ldgate = 0;
+    if (!p.has_gate) p.g.gate_values = p.g.h_out;
+    for (const void **q : {&p.g.post_weight, &p.g.post_bias, &p.g.pre_weight})
+        if (*q == nullptr) *q = p.g.h_out;
     float *const out[SUMS] = {g.d_pre_weight, g.d_pre_bias, g.d_post_weight, g.d_post_bias, d.gate == MMM_GATE_COL ? static_cast<float *>(g.d_gate) : nullptr};
-    const int64_t groups = norm_grad_groups(d.M);
+    const int64_t groups = norm_grad_groups(d.M, d.N);
     ReduceParams r{p.partials, groups, d.N, 0, {}};
     for (int q = 0; q < SUMS; ++q) {
         p.place[q] = out[q] != nullptr ? r.sums : -1;
@@ -459,13 +604,16 @@ hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_bl
     }
     p.sums = r.sums;
     (void)hipGetLastError();
-    with_types(d, [&](auto t, auto th, auto ty) {
+    with_types(p.d, [&](auto t, auto th, auto ty) {
         typedef decltype(t) T;
         typedef decltype(th) TH;
         typedef decltype(ty) TY;
-        void (*fn)(const NormGradParams) = shape.pieces == 1   ? mmm_block_norm_grad_kernel<T, TH, TY, 1>
-                                           : shape.pieces == 2 ? mmm_block_norm_grad_kernel<T, TH, TY, 2>
-                                                               : mmm_block_norm_grad_kernel<T, TH, TY, 4>;
+        const bool biases = g.d_pre_bias != nullptr || g.d_post_bias != nullptr || g.post_bias != nullptr;
+        void (*fn)(const NormGradParams) =
+            d.N < PIECE         ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 4, true, false>
+            : shape.pieces == 1 ? biases ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, true> : mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, false, true>
+            : shape.pieces == 2 ? mmm_block_norm_grad_kernel<T, TH, TY, 2, 8, true, true>
+                                : mmm_block_norm_grad_kernel<T, TH, TY, 4, 16, true, true>;
         hipLaunchKernelGGL(fn, dim3((uint32_t)groups), dim3(shape.threads), 0, s, p);
         return 0;
     });
