@@ -326,14 +326,16 @@ def mmm_epilogue_backward_workspace_bytes(M: int, N: int) -> int:
 
 def mmm_epilogue_backward(M: int, N: int, dt: int, out_dtype: int, activation: int, dC, lddc: int, Z, ldz: int, dZ, lddz: int, dbias=None,
                           workspace=None, workspace_bytes: int = 0, stream=None) -> None:
-    _check(lib.mmm_epilogue_backward(M, N, dt, out_dtype, activation, _ptr(dC), lddc, _ptr(Z), ldz, _ptr(dZ), lddz, _ptr(dbias), _ptr(workspace),
-                                     workspace_bytes, _stream(stream)), "mmm_epilogue_backward")
+    _check(native.epilogue_backward(M, N, dt, out_dtype, activation, _ptr(dC), lddc, _ptr(Z), ldz, _ptr(dZ), lddz, _ptr(dbias), _ptr(workspace),
+                                    workspace_bytes, _stream(stream)), "mmm_epilogue_backward")
 
 
 def mmm_block_norm(desc: BlockNormDesc, h, ldh: int, y, ldy: int, gate, ldgate: int, post_weight, post_bias, pre_weight, pre_bias, h_out,
                    ldh_out: int, n, ldn: int, stream=None) -> None:
-    _check(lib.mmm_block_norm(ctypes.byref(desc), _ptr(h), ldh, _ptr(y), ldy, _ptr(gate), ldgate, _ptr(post_weight), _ptr(post_bias),
-                              _ptr(pre_weight), _ptr(pre_bias), _ptr(h_out), ldh_out, _ptr(n), ldn, _stream(stream)), "mmm_block_norm")
+    d = desc
+    _check(native.block_norm(d.M, d.N, d.dt, d.dt_h, d.dt_y, d.post, d.pre, d.gate, d.eps, d.alpha, _ptr(h), ldh, _ptr(y), ldy, _ptr(gate), ldgate,
+                             _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), _ptr(h_out), ldh_out, _ptr(n), ldn,
+                             _stream(stream)), "mmm_block_norm")
 
 
 def mmm_block_norm_backward_workspace_bytes(M: int, N: int) -> int:

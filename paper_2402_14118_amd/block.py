@@ -28,6 +28,7 @@ class BlockNorm:
                  alpha: float = 1.0, eps: float = 1e-5, dtype_h: Optional[int] = None, dtype_y: Optional[int] = None, training: bool = False,
                  device="cuda:0"):
         self.desc = B.BlockNormDesc(M, N, dtype, dtype if dtype_h is None else dtype_h, dtype if dtype_y is None else dtype_y, post, pre, gate, eps, alpha)
+        self.dtype, self.dtype_h, self.dtype_y, self.shape, self.columns = dtype, self.desc.dt_h, self.desc.dt_y, (M, N), (N,)
         self.device = own_device(device)
         nbytes = B.mmm_block_norm_backward_workspace_bytes(M, N)   # (checks M and N)
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if training else None
@@ -46,12 +47,16 @@ class BlockNorm:
                 gate: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
                 pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
         """H_out may be H."""
-        d, shape = self.desc, (self.desc.M, self.desc.N)
-        check_device(self.device)
-        B.mmm_block_norm(d, *rows("H", H, shape, d.dt_h, self.device, False), *rows("Y", Y, shape, d.dt_y, self.device), *self._gate("gate", gate),
-                         self._vector("post_weight", post_weight, d.dt), self._vector("post_bias", post_bias, d.dt),
-                         self._vector("pre_weight", pre_weight, d.dt), self._vector("pre_bias", pre_bias, d.dt),
-                         *rows("H_out", H_out, shape, d.dt_h, self.device), *rows("normed", normed, shape, d.dt, self.device), stream)
+        d, dt, dev, shape = self.desc, self.dtype, self.device, self.shape
+        check_device(dev)
+        h, ldh = rows("H", H, shape, self.dtype_h, dev, False)
+        y, ldy = rows("Y", Y, shape, self.dtype_y, dev)
+        g, ldg = self._gate("gate", gate) if gate is not None else (None, 0)
+        ho, ldho = rows("H_out", H_out, shape, self.dtype_h, dev)
+        n, ldn = rows("normed", normed, shape, dt, dev)
+        pw, pb, w, b = (None if t is None else rows(name, t, self.columns, dt, dev)[0] for name, t in
+                        (("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight), ("pre_bias", pre_bias)))
+        B.mmm_block_norm(d, h, ldh, y, ldy, g, ldg, pw, pb, w, b, ho, ldho, n, ldn, stream)
 
     def backward(self, H_out: Optional[torch.Tensor] = None, grad_normed: Optional[torch.Tensor] = None, grad_H_out: Optional[torch.Tensor] = None,
                  grad_H: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,

@@ -1,5 +1,5 @@
 // CPython entry points for the calls a program makes per step (mmm_build_maps, mmm_matmul,
-// mmm_matmul_fused, mmm_matmul_epilogue).  They do what the ctypes functions of binding.py do -- marshal integers and call
+// mmm_matmul_fused, mmm_matmul_epilogue, mmm_block_norm, mmm_epilogue_backward).  They do what the ctypes functions of binding.py do -- marshal integers and call
 // the C ABI -- at 0.3 instead of about 3 us per call: a small problem is bound by the host, where a
 // kernel launch alone takes 3.5 us.  Pointers are passed as integers (None = NULL).  The GIL is
 // released around the call, as ctypes does.
@@ -146,11 +146,76 @@ PyObject *matmul_epilogue(PyObject *, PyObject *const *v, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
+// block_norm(M, N, dt, dt_h, dt_y, post, pre, gate_kind, eps, alpha, h, ldh, y, ldy, gate, ldgate, post_weight, post_bias, pre_weight, pre_bias,
+// h_out, ldh_out, n, ldn, stream)
+PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!arity("block_norm", n, 25)) return nullptr;
+    Args a{v};
+    mmm_block_norm_desc d;
+    d.M = a.num(0);
+    d.N = a.num(1);
+    d.dt = (int32_t)a.num(2);
+    d.dt_h = (int32_t)a.num(3);
+    d.dt_y = (int32_t)a.num(4);
+    d.post = (int32_t)a.num(5);
+    d.pre = (int32_t)a.num(6);
+    d.gate = (int32_t)a.num(7);
+    d.eps = a.real(8);
+    d.alpha = a.real(9);
+    const void *h = a.ptr(10);
+    const int64_t ldh = a.num(11);
+    const void *y = a.ptr(12);
+    const int64_t ldy = a.num(13);
+    const void *gate = a.ptr(14);
+    const int64_t ldgate = a.num(15);
+    const void *post_weight = a.ptr(16), *post_bias = a.ptr(17), *pre_weight = a.ptr(18), *pre_bias = a.ptr(19);
+    void *h_out = a.ptr(20);
+    const int64_t ldh_out = a.num(21);
+    void *out = a.ptr(22);
+    const int64_t ldn = a.num(23);
+    void *stream = a.ptr(24);
+    if (!a.ok) return nullptr;
+    mmm_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = mmm_block_norm(&d, h, ldh, y, ldy, gate, ldgate, post_weight, post_bias, pre_weight, pre_bias, h_out, ldh_out, out, ldn, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+// epilogue_backward(M, N, dt, out_dtype, activation, dC, lddc, Z, ldz, dZ, lddz, dbias, workspace, workspace_bytes, stream)
+PyObject *epilogue_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!arity("epilogue_backward", n, 15)) return nullptr;
+    Args a{v};
+    const int64_t M = a.num(0), N = a.num(1);
+    const mmm_dtype dt = (mmm_dtype)a.num(2), out_dtype = (mmm_dtype)a.num(3);
+    const int32_t activation = (int32_t)a.num(4);
+    const void *dC = a.ptr(5);
+    const int64_t lddc = a.num(6);
+    const void *Z = a.ptr(7);
+    const int64_t ldz = a.num(8);
+    void *dZ = a.ptr(9);
+    const int64_t lddz = a.num(10);
+    float *dbias = static_cast<float *>(a.ptr(11));
+    void *ws = a.ptr(12);
+    const size_t bytes = (size_t)a.num(13);
+    void *stream = a.ptr(14);
+    if (!a.ok) return nullptr;
+    mmm_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = mmm_epilogue_backward(M, N, dt, out_dtype, activation, dC, lddc, Z, ldz, dZ, lddz, dbias, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
 PyMethodDef methods[] = {
     {"build_maps", (PyCFunction)(void (*)(void))build_maps, METH_FASTCALL, nullptr},
     {"matmul", (PyCFunction)(void (*)(void))matmul, METH_FASTCALL, nullptr},
     {"matmul_fused", (PyCFunction)(void (*)(void))matmul_fused, METH_FASTCALL, nullptr},
     {"matmul_epilogue", (PyCFunction)(void (*)(void))matmul_epilogue, METH_FASTCALL, nullptr},
+    {"block_norm", (PyCFunction)(void (*)(void))block_norm, METH_FASTCALL, nullptr},
+    {"epilogue_backward", (PyCFunction)(void (*)(void))epilogue_backward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -19,7 +19,7 @@ def rows(name: str, t: Optional[torch.Tensor], shape, dtype: int, device, option
         return None, 0
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if t.dtype is not TORCH_TYPES.get(dtype):
+    if CODES.get(t.dtype) != dtype:
         raise TypeError(f"{name} is {t.dtype}, not {TORCH_TYPES.get(dtype)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
