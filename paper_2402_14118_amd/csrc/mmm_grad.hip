@@ -16,7 +16,6 @@
 // way, one barrier per step.  In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that
 // eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
 #include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "mmm_internal.h"
@@ -227,27 +226,24 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
             for (int n = 0; n < NR; ++n) piece_r[n] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(dc, (int)at_r[n], 0, 0));
         }
     };
-    // to half `to` of LDS
-    auto place = [&](int to) __attribute__((always_inline)) {
+    // piece n of those of L, then R, to half `to` of LDS
+    auto place = [&](int n, int to) __attribute__((always_inline)) {
         char *const at = lds[to];
-#pragma unroll
-        for (int n = 0; n < NL; ++n) {
+        if (n < NL) {
             const uint32_t row = row_l + (uint32_t)n * (NT / 8);
-            *reinterpret_cast<u32x4 *>(at + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = piece_l[n];
-        }
+            *reinterpret_cast<u32x4 *>(at + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = piece_l[n < NL ? n : 0];
+        } else if constexpr (TO_X) {
+            const int m = n - NL;
+            const uint32_t row = row_l + (uint32_t)m * (NT / 8);
+            u32x4 v = piece_r[m];
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            if constexpr (TO_X) {
-                const uint32_t row = row_l + (uint32_t)n * (NT / 8);
-                u32x4 v = piece_r[n];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = (block_bits[n] & at_r[n] & block_bit) != 0u ? v[u] : 0u;
-                *reinterpret_cast<u32x4 *>(at + TL * ROWB + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = v;
-            } else {
-                const uint32_t q = (uint32_t)tid + (uint32_t)n * NT, rho = q / PIECES, col = q % PIECES;   // col: piece of the row
-                const uint32_t turned = ESZ == 4 ? ((col >> 2) ^ (rho >> 2 & TURN)) << 2 | (col & 3u) : ((col >> 1) ^ (rho & TURN)) << 1 | (col & 1u);
-                *reinterpret_cast<u32x4 *>(at + TL * ROWB + rho * TURNED_ROW + (turned << 4)) = piece_r[n];
-            }
+            for (int u = 0; u < 4; ++u) v[u] = (block_bits[m] & at_r[m] & block_bit) != 0u ? v[u] : 0u;
+            *reinterpret_cast<u32x4 *>(at + TL * ROWB + row * ROWB + ((c_l ^ (row & 7u)) << 4)) = v;
+        } else {
+            const int m = n - NL;
+            const uint32_t q = (uint32_t)tid + (uint32_t)m * NT, rho = q / PIECES, col = q % PIECES;   // col: piece of the row
+            const uint32_t turned = ESZ == 4 ? ((col >> 2) ^ (rho >> 2 & TURN)) << 2 | (col & 3u) : ((col >> 1) ^ (rho & TURN)) << 1 | (col & 1u);
+            *reinterpret_cast<u32x4 *>(at + TL * ROWB + rho * TURNED_ROW + (turned << 4)) = piece_r[m];
         }
     };
     floatx4 acc[FR][FL];
@@ -256,7 +252,9 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
 #pragma unroll
         for (int b = 0; b < FL; ++b) acc[a][b] = floatx4{0, 0, 0, 0};
 
-    auto compute = [&](int from) __attribute__((always_inline)) {
+    // The step in half `from`; with `more` the next one's operands go to the other half between its last products: a write of 16 bytes per lane takes as long as
+    // a matrix instruction or two.
+    auto compute = [&](int from, auto more) __attribute__((always_inline)) {
         const char *const at = lds[from];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -292,20 +290,27 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
                 }
             }
 #pragma unroll
-            for (int a = 0; a < FR; ++a)
+            for (int a = 0; a < FR; ++a) {
 #pragma unroll
                 for (int b = 0; b < FL; ++b) multiply<T>(r[a], l[b], acc[a][b]);
+                if (decltype(more)::value && kk == 1)
+#pragma unroll
+                    for (int n = a * (NL + NR) / FR; n < (a + 1) * (NL + NR) / FR; ++n) place(n, from ^ 1);
+            }
         }
     };
     const int first = (int)split * p.steps_per_split, end = min(first + p.steps_per_split, p.steps);   // (no part is empty)
     fetch(first);
-    place(0);
-    for (int step = first, half = 0; step < end; ++step, half ^= 1) {
-        if (step + 1 < end) fetch(step + 1);
+#pragma unroll
+    for (int n = 0; n < NL + NR; ++n) place(n, 0);
+    int half = 0;
+    for (int step = first + 1; step < end; ++step, half ^= 1) {
+        fetch(step);
         __syncthreads();   // the step's operands are there; nobody reads the other half any more
-        compute(half);
-        if (step + 1 < end) place(half ^ 1);
+        compute(half, std::true_type{});
     }
+    __syncthreads();
+    compute(half, std::false_type{});
 
     // ---- results: a lane holds four neighbours along R of sixteen along L
     const uint64_t pitch = (size_r + 3u) & ~3u;
@@ -372,34 +377,41 @@ hipError_t clear_rows(void *out, int64_t pitch, int64_t bytes, int64_t rows, con
     return hipGetLastError();
 }
 
-// Tile and split of the contraction.  A tile of 128 x 128 feeds the matrix cores from LDS twice as well as one of 64 x 64, which leaves less of
-// small results idle and makes four times as many workgroups; where those are still few the contraction is split and the parts joined by a second launch.
-// Microseconds of a step of a workgroup where a compute unit has several (fitted, see estimate).
+// Tile and split of the contraction.  The larger a tile, the fewer operands it takes from LDS per product (256 x 256: as many cycles of LDS as of
+// matrix instructions; 64 x 64: four times as many); a smaller one leaves less of the machine and of its own edges idle.  Where there are few tiles the
+// contraction is split and the parts are joined by a second launch.  The estimate is fitted to 36 shapes of each element type, three tiles and one to 32 parts
+// (16 x 200 x 16384 to 2048 x 16384 x 4096, 2160 timings, off by 9 % of 16-bit and 5 % of float ones in the mean): its choice takes 3 and 2 % longer than the best.
+// Multiplication alone, us, 64, 128, 256: 2048 x 16384 x 4096 bf16, dX 581, 322, 252; 512 x 2048 x 2048 16, 22, 31; floats 2394, 2126, 2034 and 49, 51, 60.
+struct TileCost {
+    int tile, at_once;            // workgroups that a compute unit runs side by side
+    double fixed, alone, busy;    // microseconds: of the launch; of a step, of a workgroup by itself, and of each of many
+};
+constexpr TileCost kTiles16[] = {{64, 4, 7.5, 0.32, 0.245}, {128, 2, 9.5, 0.69, 0.60}, {256, 1, 13.6, 1.47, 1.47}};
+constexpr TileCost kTilesFloat[] = {{64, 4, 7.6, 0.72, 0.59}, {128, 2, 9.9, 2.18, 2.18}, {256, 1, 14.3, 7.57, 7.57}};
+constexpr double kJoin = 1.5, kJoinPerMB = 0.3;
+
 struct GradPlan { int tile; int32_t splits, steps_per_split; };
-double estimate(int64_t size_r, int64_t size_l, int tile, int64_t steps, bool floats, int64_t splits)
-{
-    const double tiles = (double)((size_r + tile - 1) / tile) * (double)((size_l + tile - 1) / tile), per = (double)((steps + splits - 1) / splits);
-    const double step = floats ? (tile == 128 ? 2.0 : 0.6) : (tile == 128 ? 0.70 : 0.25);
-    const double alone = floats ? (tile == 128 ? 2.0 : 1.0) : (tile == 128 ? 1.0 : 0.7);   // of a workgroup that has a compute unit to itself
-    const double rounds = tiles * (double)splits / 256.0;
-    double us = per * (rounds <= 1.0 ? alone : std::max(alone, std::ceil(rounds) * step));
-    if (splits > 1) us += 3.0 + (double)splits * (double)size_r * (double)size_l * 8.0 / 3e6;
-    return us;
-}
-GradPlan plan_grad(int64_t size_r, int64_t size_l, int64_t steps, bool floats, size_t room, size_t bytes_per_split)
+// rows_bytes: from a row of dC to the next; a tile's rows lie within 2^31 bytes
+GradPlan plan_grad(int64_t size_r, int64_t size_l, int64_t steps, bool floats, size_t room, size_t bytes_per_split, int64_t row_bytes)
 {
     GradPlan best{};
     double least = -1.0;
-    for (int tile : {128, 64})
-        for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (want > 1 && ((size_t)want * bytes_per_split > room || steps < 4 * want)) break;
+    for (const TileCost &c : floats ? kTilesFloat : kTiles16) {
+        if (c.tile > 128 && c.tile * row_bytes >= 0x80000000LL) continue;
+        const int64_t tiles = ((size_r + c.tile - 1) / c.tile) * ((size_l + c.tile - 1) / c.tile);
+        for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            if (want > 1 && ((size_t)want * bytes_per_split > room || steps < want)) break;
             const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;   // no part is empty
-            const double us = estimate(size_r, size_l, tile, steps, floats, splits);
+            const int64_t round = 256 * c.at_once, left = tiles * splits % round;
+            const double rounds = (double)(tiles * splits / round) * std::max(c.alone, c.busy * c.at_once) +
+                                  (left != 0 ? std::max(c.alone, c.busy * (double)((left + 255) / 256)) : 0.0);
+            const double us = c.fixed + (double)per * rounds + (splits > 1 ? kJoin + (double)splits * (double)size_r * (double)size_l * 4e-6 * kJoinPerMB : 0.0);
             if (least < 0.0 || us < least) {
                 least = us;
-                best = {tile, (int32_t)splits, (int32_t)per};
+                best = {c.tile, (int32_t)splits, (int32_t)per};
             }
         }
+    }
     return best;
 }
 
@@ -409,14 +421,16 @@ template <typename T, bool TO_X> hipError_t launch(const mmm_maps *m, GradParams
     // row-compacted mode: as many k as the most recent count has found (a guess: the kernels go by the number the device has)
     const int64_t live = m->b_compact && m->stats_b_valid ? std::max<int64_t>(1, std::min<int64_t>(m->K, (int64_t)m->stats_rows_b)) : m->K;
     const GradPlan plan = plan_grad(TO_X ? live : size_r, TO_X ? size_l : live, p.steps, sizeof(T) == 4, m->partial_bytes,
-                                    (size_t)((size_r + 3) & ~3LL) * (size_t)size_l * sizeof(float));
+                                    (size_t)((size_r + 3) & ~3LL) * (size_t)size_l * sizeof(float), p.lddc * (int64_t)sizeof(T));
     const int64_t tiles = ((size_r + plan.tile - 1) / plan.tile) * ((size_l + plan.tile - 1) / plan.tile) * plan.splits;
-    if (tiles > (1LL << 32) / 256 - 1) return hipErrorInvalidValue;   // threads of a launch
+    if (tiles > (1LL << 32) / 512 - 1) return hipErrorInvalidValue;   // threads of a launch
     p.splits = plan.splits;
     p.steps_per_split = plan.steps_per_split;
     p.partials = m->partials;
-    void (*fn)(const GradParams) = plan.tile == 128 ? mmm_grad_kernel<T, TO_X, 2, 2, 4, 4> : mmm_grad_kernel<T, TO_X, 2, 2, 2, 2>;
-    hipLaunchKernelGGL(fn, dim3((uint32_t)tiles), dim3(256), 0, s, p);
+    void (*fn)(const GradParams) = plan.tile == 256   ? mmm_grad_kernel<T, TO_X, 2, 4, 8, 4>
+                                   : plan.tile == 128 ? mmm_grad_kernel<T, TO_X, 2, 2, 4, 4>
+                                                      : mmm_grad_kernel<T, TO_X, 2, 2, 2, 2>;
+    hipLaunchKernelGGL(fn, dim3((uint32_t)tiles), dim3(plan.tile == 256 ? 512 : 256), 0, s, p);
     if (plan.splits > 1) {
         const dim3 grid((uint32_t)((size_r + 1023) / 1024), (uint32_t)std::min<int64_t>(size_l, 65535));
         hipLaunchKernelGGL((mmm_grad_join_kernel<T, TO_X>), grid, dim3(256), 0, s, p);

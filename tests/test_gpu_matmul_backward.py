@@ -1,7 +1,7 @@
 """The gradients of the masked product against the formulas in 64 bits, under the maps as built.
 
 Bound: a float sum of n products of exact operands is off by at most n roundings of 2^-24 of the sum of their magnitudes, whatever the order
-(floats: and one for the product); n is the length of the contraction here, at most 2048.  dX is rounded to its type once more.  Small whole numbers are exact."""
+(floats: and one for the product); n is the length of the contraction here.  dX is rounded to its type once more.  Small whole numbers are exact."""
 import pytest
 import torch
 
@@ -156,3 +156,34 @@ def test_another_stream_and_a_replayed_graph(rows):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(p.dX, want[0]) and torch.equal(p.dY, want[1])
+
+
+# sizes whose results fill 128 x 128 and 256 x 256 tiles (and the edges of them), and long contractions over few results, whose parts are joined
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,M,K,N,rows", [("bf16", 1000, 4100, 2080, None), ("f16", 2048, 2048, 1032, 0.5), ("f32", 1300, 2300, 1544, None), ("f32", 2050, 3000, 1032, 0.4),
+                                           ("bf16", 2900, 5000, 4104, None), ("bf16", 24, 70, 8192, None), ("f32", 2048, 72, 136, None), ("f16", 2000, 130, 64, 0.5)])
+def test_tiles_and_parts(dt, M, K, N, rows):
+    """The reference on the device, in 64 bits: the sizes are larger here."""
+    g = torch.Generator(device="cuda").manual_seed(M + K)
+    t = T[dt][1]
+    X, Y, dC = (torch.randn(s, generator=g, device="cuda").to(t) for s in ((M, K), (K, N), (M, N)))
+    keep = torch.rand(M, K, generator=g, device="cuda") < 0.3
+    blocks = torch.rand(K, N // 8, generator=g, device="cuda") < 0.5
+    on_rows = None if rows is None else torch.rand(1, K, generator=g, device="cuda") < rows
+    eng = mm.MaskedMatmul(M, K, N, 8, T[dt][0])
+    eng.build_maps(X, Y, keep_a=words(keep.cpu()), keep_rows=None if rows is None else words(on_rows.cpu()), keep_blocks=words(blocks.cpu()))
+    a_on = keep & (X != 0)
+    b_on = (blocks if rows is None else blocks & on_rows.view(-1, 1)).repeat_interleave(8, 1)
+    A, Bm, G = X.double() * a_on, Y.double() * b_on, dC.double()
+    half = torch.finfo(t).eps / 2
+    for counted in (False, True):
+        if counted:
+            eng.stats()   # (the number of live rows is then known to the choice of tile)
+        dX, dY = torch.full_like(X, 7.0), torch.full((K, N), 7.0, device="cuda")
+        eng.matmul_backward(X, Y, dC, dX, dY)
+        for got, want, mag, n, step in ((dX, (G @ Bm.t().contiguous()) * a_on, G.abs() @ Bm.abs().t().contiguous(), N, half),
+                                        (dY, (A.t().contiguous() @ G) * b_on, A.abs().t().contiguous() @ G.abs(), M, 0.0)):
+            assert bool(((got.double() - want).abs() <= (n + 1) * U * mag + step * want.abs() * (1 + 1e-3)).all())
+        more = dY.clone()
+        eng.matmul_backward(X, Y, dC, dY=more, accumulate=True)
+        assert torch.equal(more, dY + dY)
