@@ -24,6 +24,8 @@ __global__ __launch_bounds__(256) void mmm_splitk_epilogue_kernel(const E *P, vo
     columns.load(epilogue, (int64_t)col * VEC);
     for (uint32_t row = blockIdx.y; row < M; row += gridDim.y) {
         const int64_t e = (int64_t)row * NV + col;
+        E more[VEC];
+        columns.residual(epilogue, row, (int64_t)col * VEC, more);
         vec sum = parts[e];
         for (int32_t sp = 1; sp < splits; sp += 8) {
             vec v[8];
@@ -36,7 +38,8 @@ __global__ __launch_bounds__(256) void mmm_splitk_epilogue_kernel(const E *P, vo
         E z[VEC];
 #pragma unroll
         for (int q = 0; q < VEC; ++q) z[q] = sum[q];
-        columns.finish(epilogue, z, C, ldc, row, (int64_t)col * VEC);
+        columns.activate(epilogue, z, row, (int64_t)col * VEC);
+        columns.finish(epilogue, z, more, C, ldc, row, (int64_t)col * VEC);
     }
 }
 

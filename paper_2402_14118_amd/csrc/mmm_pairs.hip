@@ -387,6 +387,14 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
         if constexpr (FUSED) __builtin_amdgcn_s_waitcnt(0);   // nothing is under way at the start of a trip (else the first one waits for what might be)
     }
 
+    const uint32_t col = col0 + (uint32_t)(g * BW + part * C16 + entry);
+    mmm_column_values<typename Elem<T>::model, acc_t, 1> column;
+    acc_t more[1];
+    if constexpr (EPI)   // (asked for here, while sums are exchanged)
+        if (ks == 0 && col < p.N) {
+            column.load(p.epilogue, col);
+            column.residual(p.epilogue, row_i, col, more);
+        }
     // The lanes of a group that hold the same columns exchange halves of them: one column per lane is left.
 #pragma unroll
     for (int half = C16 / 2, stride = BW / 2; half >= 1; half /= 2, stride /= 2) {
@@ -397,7 +405,6 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
             acc[q] = (upper ? acc[q + half] : acc[q]) + __shfl_xor(send, stride, 64);
         }
     }
-    const uint32_t col = col0 + (uint32_t)(g * BW + part * C16 + entry);
     if (KS > 1) {   // add the partial sums of the waves that shared this column span, in wave order
         if (ks > 0) red[((ks - 1) * CW + cw) * 64 + lane] = acc[0];
         __syncthreads();
@@ -407,10 +414,9 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
     }
     if (ks == 0 && col < p.N) {
         if constexpr (EPI) {
-            const acc_t sum[1] = {acc[0]};
-            mmm_column_values<typename Elem<T>::model, acc_t, 1> column;
-            column.load(p.epilogue, col);
-            column.finish(p.epilogue, sum, p.C, p.ldc, row_i, col);
+            acc_t z[1] = {acc[0]};
+            column.activate(p.epilogue, z, row_i, col);
+            column.finish(p.epilogue, z, more, p.C, p.ldc, row_i, col);
         } else {
             acc_t *dst = static_cast<acc_t *>(p.C) + (int64_t)row_i * p.ldc + col;
             *dst = p.accumulate ? *dst + acc[0] : acc[0];
