@@ -314,8 +314,8 @@ def mmm_matmul_epilogue(maps: int, dt: int, X, ldx: int, ma: Optional[MaskA], Y,
 
 def mmm_matmul_backward(maps: int, dt: int, X, ldx: int, Y, ldy: int, dC, lddc: int, dX, lddx: int, dY, lddy: int, accumulate: int = 0,
                         all_x: int = 0, stream=None) -> None:
-    _check(lib.mmm_matmul_backward(maps, dt, _ptr(X), ldx, _ptr(Y), ldy, _ptr(dC), lddc, _ptr(dX), lddx, _ptr(dY), lddy, int(accumulate), int(all_x),
-                                   _stream(stream)), "mmm_matmul_backward")
+    _check(native.matmul_backward(maps, dt, _ptr(X), ldx, _ptr(Y), ldy, _ptr(dC), lddc, _ptr(dX), lddx, _ptr(dY), lddy, int(accumulate), int(all_x),
+                                  _stream(stream)), "mmm_matmul_backward")
 
 
 def mmm_epilogue_backward_workspace_bytes(M: int, N: int) -> int:

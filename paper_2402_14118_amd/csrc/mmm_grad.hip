@@ -353,13 +353,22 @@ template <typename T, bool TO_X> __global__ __launch_bounds__(256) void mmm_grad
     }
 }
 
-// Zeros: rows of `bytes` bytes, those of the bitmap's zero bits where there is one.  16 bytes per lane.
-__global__ __launch_bounds__(256) void mmm_clear_rows_kernel(char *out, int64_t pitch, int64_t bytes, int64_t rows, const uint64_t *kept)
+// Row-compacted mode: zeros where no tile writes, in one launch.  dX: everything (its results lie here and there in its rows); dY: the rows
+// that are off.
+struct ClearParams {
+    char *dX, *dY;   // null: not asked for
+    int64_t dx_pitch, dx_bytes, M, dy_pitch, dy_bytes, K;
+    const uint64_t *rows;
+};
+__global__ __launch_bounds__(256) void mmm_grad_clear_kernel(const ClearParams p)
 {
     typedef AnyPiece<2>::type piece_any;
     typedef uint16_t half_any __attribute__((may_alias));
+    const bool of_y = blockIdx.z != 0 || p.dX == nullptr;
+    char *const out = of_y ? p.dY : p.dX;
+    const int64_t pitch = of_y ? p.dy_pitch : p.dx_pitch, bytes = of_y ? p.dy_bytes : p.dx_bytes, rows = of_y ? p.K : p.M;
     for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-        if (kept != nullptr && (kept[row >> 6] >> (row & 63) & 1ull)) continue;
+        if (of_y && (p.rows[row >> 6] >> (row & 63) & 1ull)) continue;
         for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16; at < bytes; at += (int64_t)gridDim.x * 256 * 16) {
             char *const to = out + row * pitch + at;
             if (at + 16 <= bytes)
@@ -368,13 +377,6 @@ __global__ __launch_bounds__(256) void mmm_clear_rows_kernel(char *out, int64_t 
                 for (int64_t q = 0; at + q < bytes; q += 2) *reinterpret_cast<half_any *>(to + q) = 0;
         }
     }
-}
-
-hipError_t clear_rows(void *out, int64_t pitch, int64_t bytes, int64_t rows, const uint64_t *kept, hipStream_t s)
-{
-    const dim3 grid((uint32_t)std::min<int64_t>((bytes + 4095) / 4096, 64), (uint32_t)std::min<int64_t>(rows, 65535));
-    hipLaunchKernelGGL(mmm_clear_rows_kernel, grid, dim3(256), 0, s, static_cast<char *>(out), pitch, bytes, rows, kept);
-    return hipGetLastError();
 }
 
 // Tile and split of the contraction.  The larger a tile, the fewer operands it takes from LDS per product (256 x 256: as many cycles of LDS as of
@@ -464,9 +466,15 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
     p.parts = m->a_form == MMM_FORM_PARTS;
     const int64_t esz = dtype == MMM_F32 ? 4 : 2;
     (void)hipGetLastError();
+    const bool clear_y = dY != nullptr && !accumulate;
+    if (m->b_compact && (dX != nullptr || clear_y)) {
+        const ClearParams c{static_cast<char *>(dX), clear_y ? reinterpret_cast<char *>(dY) : nullptr, lddx * esz, m->K * esz, m->M, lddy * 4, m->N * 4, m->K, m->rows_copy};
+        const int64_t bytes = std::max(dX != nullptr ? c.dx_bytes : 0, clear_y ? c.dy_bytes : 0), rows = std::max(dX != nullptr ? c.M : 0, clear_y ? c.K : 0);
+        const dim3 grid((uint32_t)std::min<int64_t>((bytes + 4095) / 4096, 16), (uint32_t)std::min<int64_t>(rows, 8192), dX != nullptr && clear_y ? 2 : 1);
+        hipLaunchKernelGGL(mmm_grad_clear_kernel, grid, dim3(256), 0, s, c);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     if (dX != nullptr) {
-        if (m->b_compact)
-            if (hipError_t e = clear_rows(dX, lddx * esz, m->K * esz, m->M, nullptr, s); e != hipSuccess) return e;
         p.out = dX;
         p.ldo = lddx;
         p.steps = (int32_t)((m->N * esz + ROWB - 1) / ROWB);
@@ -474,8 +482,6 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
         if (e != hipSuccess) return e;
     }
     if (dY != nullptr) {
-        if (m->b_compact && !accumulate)
-            if (hipError_t e = clear_rows(dY, lddy * 4, m->N * 4, m->K, m->rows_copy, s); e != hipSuccess) return e;
         p.out = dY;
         p.ldo = lddy;
         p.steps = (int32_t)(m->MBA * (dtype == MMM_F32 ? 2 : 1));

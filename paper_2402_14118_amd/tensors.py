@@ -17,18 +17,19 @@ def rows(name: str, t: Optional[torch.Tensor], shape, dtype: int, device, option
         if not optional:
             raise ValueError(f"{name} is needed")
         return None, 0
+    ld = B.native.leading(t, shape, TORCH_TYPES.get(dtype), device)
+    if ld >= 0:
+        return t, ld
+    # what is wrong with it
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} is not a tensor")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if CODES.get(t.dtype) != dtype:
         raise TypeError(f"{name} is {t.dtype}, not {TORCH_TYPES.get(dtype)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"the elements of {name} are not neighbours in memory")
-    if len(shape) == 1:
-        return t, 0
-    return t, (strides[0] if shape[0] > 1 else max(strides[0], shape[1]))
+    raise ValueError(f"the elements of {name} are not neighbours in memory")
 
 
 def own_device(device) -> torch.device:
