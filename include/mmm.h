@@ -372,7 +372,7 @@ typedef struct {
 
 /* C = act(A x B + bias) + residual.  With ma == NULL the product is that of mmm_matmul, and everything said there about X, Y and the
  * maps holds; with ma it is that of mmm_matmul_fused (the mask evaluated inside the multiplication; only the B side of the maps is
- * used; meant for few rows).  The sums are those of these calls: kernel, plan and order are the same, so that C rounded to
+ * used; meant for few rows with many zeros: a dense X is multiplied faster by MMM_PATH_MATRIX, from maps).  The sums are those of these calls: kernel, plan and order are the same, so that C rounded to
  * float is theirs bit by bit where nothing is done in the epilogue.  Rows of A and columns of B without any product give act(bias) + residual.
  * The activation and all that follows are computed in the type of the sums, whatever out_dtype is.
  * Partial sums of a split K lie in the workspace of the maps, as mmm_matmul's: two calls on one handle that may run at the same time race.

@@ -94,14 +94,19 @@ class MaskedMlp:
 
     W1 (width x hidden) and W2 (hidden x width) are masked in blocks of their rows (a block that holds only zeros is off, and learns nothing); rows of W2 (hidden units) may be selected by context.  The
     holder owns the maps of both products, the activations between them and, with training=True, the gradients on the way and the
-    workspaces of backward(): two calls that may run at the same time need a holder each.  fused (few rows, not for training): both products
-    evaluate their masks themselves, one launch each."""
+    workspaces of backward(): two calls that may run at the same time need a holder each.  fused (few rows of ReLU activations, not for
+    training): the second product evaluates their mask itself, in one launch.
+
+    A dense operand is multiplied by the matrix kernel (4 x 4096 x 16384 bf16, all blocks on: 29 us with its build, 109 by the pair kernel); for
+    ReLU's zeros the choice of kernel goes by count(), once there has been one."""
 
     def __init__(self, M: int, width: int, hidden: int, block_width: int = 32, dtype: int = B.MMM_BF16, activation: int = B.MMM_ACT_RELU,
                  post: int = B.MMM_NORM_RMS, pre: int = B.MMM_NORM_RMS, gate: int = B.MMM_GATE_NONE, alpha: float = 1.0, eps: float = 1e-5,
                  dtype_h: Optional[int] = None, fused: bool = False, training: bool = False, device="cuda:0"):
         if fused and training:
-            raise ValueError("the gradients need the maps of the activations, which fused products do not make")
+            raise ValueError("the gradients need the maps of the activations, which a fused product does not make")
+        if fused and activation != B.MMM_ACT_RELU:
+            raise ValueError("a fused product is for activations with many zeros, those of ReLU")
         self.M, self.width, self.hidden, self.dtype, self.activation, self.fused, self.training = M, width, hidden, dtype, activation, fused, training
         self.device = own_device(device)
         self.up = MaskedMatmul(M, width, hidden, block_width, dtype, self.device)
@@ -109,6 +114,9 @@ class MaskedMlp:
         self.norm = BlockNorm(M, width, dtype, post, pre, gate, alpha, eps, dtype_h, training=training, device=self.device)
         # zeros of ReLU are told by the sign, those of a smooth activation by the value
         self.pred = B.MMM_PRED_GT if activation == B.MMM_ACT_RELU else B.MMM_PRED_NONZERO
+        self.up.set_path(B.MMM_PATH_MATRIX)
+        if activation != B.MMM_ACT_RELU:
+            self.down.set_path(B.MMM_PATH_MATRIX)
 
         def room(*shape, t=None):
             return torch.empty(shape, dtype=TORCH_TYPES[dtype if t is None else t], device=self.device)
@@ -136,12 +144,10 @@ class MaskedMlp:
         self.up.build_maps(None, W1, keep_blocks=keep_blocks1, stream=stream)
         self.down.build_maps(None, W2, keep_rows=keep_rows2, keep_blocks=keep_blocks2, stream=stream)
 
-    def _product(self, eng, X, Y, C, pred, stream, **epilogue):
-        if self.fused:
-            eng.matmul_epilogue(X, Y, C, pred=pred, stream=stream, **epilogue)
-        else:
-            eng.build_maps(X, None, pred, stream=stream)
-            eng.matmul_epilogue(X, Y, C, stream=stream, **epilogue)
+    def count(self, stream=None):
+        """Count the densities of the last forward call (waits for the stream): what the choice of kernel, of tiles and of the form of floats goes by
+        from then on.  Returns ((non-zeros, blocks, products) of the first product, the same of the second; None where its mask is fused)."""
+        return self.up.stats(stream), None if self.fused else self.down.stats(stream)
 
     def forward(self, N: torch.Tensor, H: torch.Tensor, H_out: torch.Tensor, normed: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
                 post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None, pre_weight: Optional[torch.Tensor] = None,
@@ -151,8 +157,11 @@ class MaskedMlp:
             raise ValueError("set_weights() comes first")
         rows("N", N, (self.M, self.width), self.dtype, self.device, False)
         kept = self.preact if self.training and self.preact is not self.a else None
-        self._product(self.up, N, self.W1, self.a, B.MMM_PRED_NONZERO, stream, bias=self.b1, activation=self.activation, preact=kept)
-        self._product(self.down, self.a, self.W2, self.y, self.pred, stream, bias=self.b2)
+        self.up.build_maps(N, None, stream=stream)
+        self.up.matmul_epilogue(N, self.W1, self.a, bias=self.b1, activation=self.activation, preact=kept, stream=stream)
+        if not self.fused:
+            self.down.build_maps(self.a, None, self.pred, stream=stream)
+        self.down.matmul_epilogue(self.a, self.W2, self.y, bias=self.b2, pred=self.pred if self.fused else None, stream=stream)
         self.norm.forward(H, normed=normed, H_out=H_out, Y=self.y, gate=gate, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight,
                           pre_bias=pre_bias, stream=stream)
 

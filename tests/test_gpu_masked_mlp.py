@@ -97,7 +97,7 @@ def test_training_step(dt, act, context):
 @pytest.mark.gpu
 @pytest.mark.parametrize("M", [1, 5])
 def test_decode(M):
-    """Few rows: masks evaluated inside the products, the stream in place and in float beside 16-bit weights."""
+    """Few rows: the mask evaluated inside the second product, the stream in place and in float beside 16-bit weights."""
     mlp, d, ref, on1, on2 = setup("bf16", "relu", M=M, context=False, fused=True, dtype_h=mm.MMM_F32)
     stream, n = d["H"].float(), torch.empty_like(d["N"])
     mlp.forward(d["N"], stream, stream, n, gate=d["gate"], post_weight=d["post_weight"], pre_weight=d["pre_weight"], pre_bias=d["pre_bias"])
@@ -115,4 +115,23 @@ def test_order_of_calls():
     with pytest.raises(ValueError):
         mm.MaskedMlp(4, 64, 64, fused=True, training=True)
     with pytest.raises(ValueError):
+        mm.MaskedMlp(4, 64, 64, fused=True, activation=mm.MMM_ACT_SILU)
+    with pytest.raises(ValueError):
         mm.MaskedMlp(4, 64, 64).forward(d["N"][:4], d["H"][:4], out[:4])
+
+
+@pytest.mark.gpu
+def test_counted():
+    """After count() floats may come in parts and another kernel may run: the same block within the bounds."""
+    mlp, d, ref, on1, on2 = setup("f32", "relu", M=300, d=512, f=1024, context=False)
+    values = {k: d[k] for k in ("gate", "post_weight", "pre_weight", "pre_bias")}
+    first, second, n = torch.empty_like(d["H"]), torch.empty_like(d["H"]), torch.empty_like(d["H"])
+    mlp.forward(d["N"], d["H"], first, n, **values)
+    up, down = mlp.count()
+    a = torch.relu(ref["N"].detach() @ (ref["W1"].detach() * on1) + ref["b1"].detach())
+    assert up[0] == int((d["N"] != 0).sum()) and abs(down[0] - int((a > 0).sum())) <= 4      # (a unit whose argument is next to zero)
+    mlp.set_weights(d["W1"], d["W2"], d["b1"], d["b2"])
+    mlp.forward(d["N"], d["H"], first, n, **values)
+    mlp.count()
+    mlp.forward(d["N"], d["H"], second, n, **values)
+    close(second, first.double().cpu(), "f32", "H_out")
