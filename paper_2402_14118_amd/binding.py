@@ -56,6 +56,10 @@ class BlockNormDesc(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("dt", ctypes.c_int32), ("dt_h", ctypes.c_int32), ("dt_y", ctypes.c_int32),
                 ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate", ctypes.c_int32), ("eps", ctypes.c_float), ("alpha", ctypes.c_float)]
 
+    def fields(self):
+        """As the native entry points take it."""
+        return tuple(getattr(self, name) for name, _ in self._fields_)
+
 
 class BlockNormGrads(ctypes.Structure):
     _fields_ = [("h_out", ctypes.c_void_p), ("ldh_out", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
@@ -332,10 +336,8 @@ def mmm_epilogue_backward(M: int, N: int, dt: int, out_dtype: int, activation: i
 
 def mmm_block_norm(desc: BlockNormDesc, h, ldh: int, y, ldy: int, gate, ldgate: int, post_weight, post_bias, pre_weight, pre_bias, h_out,
                    ldh_out: int, n, ldn: int, stream=None) -> None:
-    d = desc
-    _check(native.block_norm(d.M, d.N, d.dt, d.dt_h, d.dt_y, d.post, d.pre, d.gate, d.eps, d.alpha, _ptr(h), ldh, _ptr(y), ldy, _ptr(gate), ldgate,
-                             _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight), _ptr(pre_bias), _ptr(h_out), ldh_out, _ptr(n), ldn,
-                             _stream(stream)), "mmm_block_norm")
+    _check(native.block_norm(desc.fields(), _ptr(h), ldh, _ptr(y), ldy, _ptr(gate), ldgate, _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight),
+                             _ptr(pre_bias), _ptr(h_out), ldh_out, _ptr(n), ldn, _stream(stream)), "mmm_block_norm")
 
 
 def mmm_block_norm_backward_workspace_bytes(M: int, N: int) -> int:

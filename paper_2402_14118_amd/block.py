@@ -32,6 +32,8 @@ class BlockNorm:
         self.device = own_device(device)
         nbytes = B.mmm_block_norm_backward_workspace_bytes(M, N)   # (checks M and N)
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if training else None
+        self.room = (self.workspace.data_ptr(), nbytes) if training else (None, 0)
+        self.fields = self.desc.fields()
 
     def _gate(self, name, t, sums=False):
         d = self.desc
@@ -40,14 +42,11 @@ class BlockNorm:
             raise ValueError(f"{name} is given, but there is no gate")
         return rows(name, t, shape, B.MMM_F32 if sums and d.gate != B.MMM_GATE_FULL else d.dt, self.device)
 
-    def _vector(self, name, t, dtype):
-        return rows(name, t, (self.desc.N,), dtype, self.device)[0]
-
     def forward(self, H: torch.Tensor, normed: Optional[torch.Tensor] = None, H_out: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
                 gate: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
                 pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
         """H_out may be H."""
-        d, dt, dev, shape = self.desc, self.dtype, self.device, self.shape
+        dt, dev, shape = self.dtype, self.device, self.shape
         check_device(dev)
         h, ldh = rows("H", H, shape, self.dtype_h, dev, False)
         y, ldy = rows("Y", Y, shape, self.dtype_y, dev)
@@ -56,7 +55,7 @@ class BlockNorm:
         n, ldn = rows("normed", normed, shape, dt, dev)
         pw, pb, w, b = (None if t is None else rows(name, t, self.columns, dt, dev)[0] for name, t in
                         (("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight), ("pre_bias", pre_bias)))
-        B.mmm_block_norm(d, h, ldh, y, ldy, g, ldg, pw, pb, w, b, ho, ldho, n, ldn, stream)
+        B._check(B.native.block_norm(self.fields, h, ldh, y, ldy, g, ldg, pw, pb, w, b, ho, ldho, n, ldn, B._stream(stream)), "mmm_block_norm")
 
     def backward(self, H_out: Optional[torch.Tensor] = None, grad_normed: Optional[torch.Tensor] = None, grad_H_out: Optional[torch.Tensor] = None,
                  grad_H: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
@@ -66,23 +65,23 @@ class BlockNorm:
                  grad_pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
         """H_out: as the forward call left it (H where there was no block).  grad_H may be grad_H_out.  Gradients that are not given are
         not worked out; those of weights, biases and of a gate per row or column are float."""
-        d, shape, f = self.desc, (self.desc.M, self.desc.N), B.MMM_F32
-        p = B._ptr
-        check_device(self.device)
-        ho, ldho = rows("H_out", H_out, shape, d.dt_h, self.device)
-        y, ldy = rows("Y", Y, shape, d.dt_y, self.device)
-        ga, ldga = self._gate("gate", gate)
-        dn, lddn = rows("grad_normed", grad_normed, shape, d.dt, self.device)
-        dho, lddho = rows("grad_H_out", grad_H_out, shape, d.dt_h, self.device)
-        dh, lddh = rows("grad_H", grad_H, shape, d.dt_h, self.device)
-        dy, lddy = rows("grad_Y", grad_Y, shape, d.dt_y, self.device)
-        dg, lddg = self._gate("grad_gate", grad_gate, sums=True)
-        g = B.BlockNormGrads(p(ho), ldho, p(y), ldy, p(ga), ldga, p(self._vector("post_weight", post_weight, d.dt)),
-                             p(self._vector("post_bias", post_bias, d.dt)), p(self._vector("pre_weight", pre_weight, d.dt)), p(dn), lddn, p(dho), lddho,
-                             p(dh), lddh, p(dy), lddy, p(dg), lddg, p(self._vector("grad_post_weight", grad_post_weight, f)),
-                             p(self._vector("grad_post_bias", grad_post_bias, f)), p(self._vector("grad_pre_weight", grad_pre_weight, f)),
-                             p(self._vector("grad_pre_bias", grad_pre_bias, f)))
-        B.mmm_block_norm_backward(d, g, self.workspace, 0 if self.workspace is None else self.workspace.numel(), stream)
+        dt, dev, shape, columns, f = self.dtype, self.device, self.shape, self.columns, B.MMM_F32
+        check_device(dev)
+        ho, ldho = rows("H_out", H_out, shape, self.dtype_h, dev)
+        y, ldy = rows("Y", Y, shape, self.dtype_y, dev)
+        ga, ldga = self._gate("gate", gate) if gate is not None else (None, 0)
+        dn, lddn = rows("grad_normed", grad_normed, shape, dt, dev)
+        dho, lddho = rows("grad_H_out", grad_H_out, shape, self.dtype_h, dev)
+        dh, lddh = rows("grad_H", grad_H, shape, self.dtype_h, dev)
+        dy, lddy = rows("grad_Y", grad_Y, shape, self.dtype_y, dev)
+        dg, lddg = self._gate("grad_gate", grad_gate, sums=True) if grad_gate is not None else (None, 0)
+        pw, pb, w = (None if t is None else rows(name, t, columns, dt, dev)[0] for name, t in
+                     (("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight)))
+        sums = (None if t is None else rows(name, t, columns, f, dev)[0] for name, t in
+                (("grad_post_weight", grad_post_weight), ("grad_post_bias", grad_post_bias), ("grad_pre_weight", grad_pre_weight),
+                 ("grad_pre_bias", grad_pre_bias)))
+        B._check(B.native.block_norm_backward(self.fields, ho, ldho, y, ldy, ga, ldga, pw, pb, w, dn, lddn, dho, lddho, dh, lddh, dy, lddy, dg, lddg, *sums,
+                                              *self.room, B._stream(stream)), "mmm_block_norm_backward")
 
 
 class MaskedMlp:

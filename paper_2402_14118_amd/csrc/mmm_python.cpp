@@ -1,5 +1,6 @@
 // CPython entry points for the calls a program makes per step (mmm_build_maps, mmm_matmul,
-// mmm_matmul_fused, mmm_matmul_epilogue, mmm_matmul_backward, mmm_block_norm, mmm_epilogue_backward).  They do what the ctypes functions of binding.py do -- marshal integers and call
+// mmm_matmul_fused, mmm_matmul_epilogue, mmm_matmul_backward, mmm_block_norm, mmm_epilogue_backward,
+// mmm_block_norm_backward).  They do what the ctypes functions of binding.py do -- marshal integers and call
 // the C ABI -- at 0.3 instead of about 3 us per call: a small problem is bound by the host, where a
 // kernel launch alone takes 3.5 us.  Pointers are passed as integers (None = NULL).  The GIL is
 // released around the call, as ctypes does.
@@ -146,13 +147,14 @@ PyObject *matmul_epilogue(PyObject *, PyObject *const *v, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
-// block_norm(M, N, dt, dt_h, dt_y, post, pre, gate_kind, eps, alpha, h, ldh, y, ldy, gate, ldgate, post_weight, post_bias, pre_weight, pre_bias,
-// h_out, ldh_out, n, ldn, stream)
-PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
+// A mmm_block_norm_desc from (M, N, dt, dt_h, dt_y, post, pre, gate, eps, alpha).
+bool description(PyObject *t, mmm_block_norm_desc &d)
 {
-    if (!arity("block_norm", n, 25)) return nullptr;
-    Args a{v};
-    mmm_block_norm_desc d;
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 10) {
+        PyErr_SetString(PyExc_TypeError, "the description of a norm has ten fields");
+        return false;
+    }
+    Args a{&PyTuple_GET_ITEM(t, 0)};
     d.M = a.num(0);
     d.N = a.num(1);
     d.dt = (int32_t)a.num(2);
@@ -163,18 +165,28 @@ PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
     d.gate = (int32_t)a.num(7);
     d.eps = a.real(8);
     d.alpha = a.real(9);
-    const void *h = a.ptr(10);
-    const int64_t ldh = a.num(11);
-    const void *y = a.ptr(12);
-    const int64_t ldy = a.num(13);
-    const void *gate = a.ptr(14);
-    const int64_t ldgate = a.num(15);
-    const void *post_weight = a.ptr(16), *post_bias = a.ptr(17), *pre_weight = a.ptr(18), *pre_bias = a.ptr(19);
-    void *h_out = a.ptr(20);
-    const int64_t ldh_out = a.num(21);
-    void *out = a.ptr(22);
-    const int64_t ldn = a.num(23);
-    void *stream = a.ptr(24);
+    return a.ok;
+}
+
+// block_norm(description, h, ldh, y, ldy, gate, ldgate, post_weight, post_bias, pre_weight, pre_bias, h_out, ldh_out, n, ldn, stream)
+PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!arity("block_norm", n, 16)) return nullptr;
+    mmm_block_norm_desc d;
+    if (!description(v[0], d)) return nullptr;
+    Args a{v};
+    const void *h = a.ptr(1);
+    const int64_t ldh = a.num(2);
+    const void *y = a.ptr(3);
+    const int64_t ldy = a.num(4);
+    const void *gate = a.ptr(5);
+    const int64_t ldgate = a.num(6);
+    const void *post_weight = a.ptr(7), *post_bias = a.ptr(8), *pre_weight = a.ptr(9), *pre_bias = a.ptr(10);
+    void *h_out = a.ptr(11);
+    const int64_t ldh_out = a.num(12);
+    void *out = a.ptr(13);
+    const int64_t ldn = a.num(14);
+    void *stream = a.ptr(15);
     if (!a.ok) return nullptr;
     mmm_status st;
     Py_BEGIN_ALLOW_THREADS
@@ -236,17 +248,61 @@ PyObject *matmul_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
-// leading(tensor, shape, dtype, device): the leading dimension of a matrix (0: of a vector) that has this shape, type and device and whose elements are
-// neighbours; -1 where anything differs (the caller then says what).  The checks of a call with nine tensors are 2 us here and 5 in Python.
-PyObject *leading(PyObject *, PyObject *const *v, Py_ssize_t n)
+// block_norm_backward(description, h_out, ldh_out, y, ldy, gate, ldgate, post_weight, post_bias, pre_weight, d_n, ldd_n, d_h_out, ldd_h_out, d_h, ldd_h,
+// d_y, ldd_y, d_gate, ldd_gate, d_post_weight, d_post_bias, d_pre_weight, d_pre_bias, workspace, workspace_bytes, stream)
+PyObject *block_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
-    if (!arity("leading", n, 4)) return nullptr;
+    if (!arity("block_norm_backward", n, 27)) return nullptr;
+    mmm_block_norm_desc d;
+    if (!description(v[0], d)) return nullptr;
+    Args a{v};
+    mmm_block_norm_grads g;
+    g.h_out = a.ptr(1);
+    g.ldh_out = a.num(2);
+    g.y = a.ptr(3);
+    g.ldy = a.num(4);
+    g.gate_values = a.ptr(5);
+    g.ldgate = a.num(6);
+    g.post_weight = a.ptr(7);
+    g.post_bias = a.ptr(8);
+    g.pre_weight = a.ptr(9);
+    g.d_n = a.ptr(10);
+    g.ldd_n = a.num(11);
+    g.d_h_out = a.ptr(12);
+    g.ldd_h_out = a.num(13);
+    g.d_h = a.ptr(14);
+    g.ldd_h = a.num(15);
+    g.d_y = a.ptr(16);
+    g.ldd_y = a.num(17);
+    g.d_gate = a.ptr(18);
+    g.ldd_gate = a.num(19);
+    g.d_post_weight = static_cast<float *>(a.ptr(20));
+    g.d_post_bias = static_cast<float *>(a.ptr(21));
+    g.d_pre_weight = static_cast<float *>(a.ptr(22));
+    g.d_pre_bias = static_cast<float *>(a.ptr(23));
+    void *ws = a.ptr(24);
+    const size_t bytes = (size_t)a.num(25);
+    void *stream = a.ptr(26);
+    if (!a.ok) return nullptr;
+    mmm_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = mmm_block_norm_backward(&d, &g, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+// place(tensor, shape, dtype, device): (address, leading dimension) of a matrix (leading dimension 0: of a vector) that has this shape, type and device
+// and whose elements are neighbours; None where anything differs (the caller then says what).
+PyObject *place(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (!arity("place", n, 4)) return nullptr;
     static PyObject *const shape_name = PyUnicode_InternFromString("shape"), *const dtype_name = PyUnicode_InternFromString("dtype"),
-                           *const device_name = PyUnicode_InternFromString("device"), *const stride_name = PyUnicode_InternFromString("stride");
+                           *const device_name = PyUnicode_InternFromString("device"), *const stride_name = PyUnicode_InternFromString("stride"),
+                           *const address_name = PyUnicode_InternFromString("data_ptr");
     PyObject *const t = v[0], *const want = v[1];
     long long ld = -1;
     PyObject *const shape = PyObject_GetAttr(t, shape_name), *const dtype = PyObject_GetAttr(t, dtype_name), *const device = PyObject_GetAttr(t, device_name);
-    PyObject *stride = nullptr;
+    PyObject *stride = nullptr, *address = nullptr;
     if (shape != nullptr && device != nullptr && PyTuple_Check(shape) && PyTuple_Check(want) && dtype == v[2]) {
         const Py_ssize_t dims = PyTuple_GET_SIZE(want);
         bool same = (dims == 1 || dims == 2) && PyTuple_GET_SIZE(shape) == dims;
@@ -260,13 +316,24 @@ PyObject *leading(PyObject *, PyObject *const *v, Py_ssize_t n)
             const long long last = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, dims - 1)), first = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0));
             if (last == 1 || size[dims - 1] <= 1) ld = dims == 1 ? 0 : size[0] > 1 || first > size[1] ? first : size[1];
         }
+        if (ld >= 0) address = PyObject_CallMethodNoArgs(t, address_name);
     }
     Py_XDECREF(shape);
     Py_XDECREF(dtype);
     Py_XDECREF(device);
     Py_XDECREF(stride);
-    if (PyErr_Occurred()) PyErr_Clear();
-    return PyLong_FromLongLong(ld < 0 ? -1 : ld);
+    PyErr_Clear();
+    if (address == nullptr) Py_RETURN_NONE;
+    PyObject *const both = PyTuple_New(2), *const leading = PyLong_FromLongLong(ld);
+    if (both == nullptr || leading == nullptr) {
+        Py_XDECREF(both);
+        Py_XDECREF(leading);
+        Py_DECREF(address);
+        return nullptr;
+    }
+    PyTuple_SET_ITEM(both, 0, address);
+    PyTuple_SET_ITEM(both, 1, leading);
+    return both;
 }
 
 PyMethodDef methods[] = {
@@ -277,7 +344,8 @@ PyMethodDef methods[] = {
     {"block_norm", (PyCFunction)(void (*)(void))block_norm, METH_FASTCALL, nullptr},
     {"epilogue_backward", (PyCFunction)(void (*)(void))epilogue_backward, METH_FASTCALL, nullptr},
     {"matmul_backward", (PyCFunction)(void (*)(void))matmul_backward, METH_FASTCALL, nullptr},
-    {"leading", (PyCFunction)(void (*)(void))leading, METH_FASTCALL, nullptr},
+    {"block_norm_backward", (PyCFunction)(void (*)(void))block_norm_backward, METH_FASTCALL, nullptr},
+    {"place", (PyCFunction)(void (*)(void))place, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -75,9 +75,8 @@ class MaskedMatmul:
         r, ldr = rows("residual", residual, shape, out, dev)
         z, ldp = rows("preact", preact, shape, out, dev)
         b = rows("bias", bias, (self.N,), dt, dev)[0]
-        B._check(B.native.matmul_epilogue(self.maps, dt, x.data_ptr(), ldx, pred is not None, 0 if pred is None else pred, threshold, B._ptr(keep_a),
-                                          y.data_ptr(), ldy, c.data_ptr(), ldc, activation, out, B._ptr(b), B._ptr(r), ldr, B._ptr(z), ldp,
-                                          B._stream(stream)), "mmm_matmul_epilogue")
+        B._check(B.native.matmul_epilogue(self.maps, dt, x, ldx, pred is not None, 0 if pred is None else pred, threshold, B._ptr(keep_a), y, ldy, c, ldc,
+                                          activation, out, b, r, ldr, z, ldp, B._stream(stream)), "mmm_matmul_epilogue")
 
     def matmul_backward(self, X: torch.Tensor, Y: torch.Tensor, dC: torch.Tensor, dX: Optional[torch.Tensor] = None,
                         dY: Optional[torch.Tensor] = None, accumulate: bool = False, all_x: bool = False, stream=None) -> None:

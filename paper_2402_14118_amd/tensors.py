@@ -12,14 +12,14 @@ CODES = {t: code for code, t in TORCH_TYPES.items()}
 
 
 def rows(name: str, t: Optional[torch.Tensor], shape, dtype: int, device, optional: bool = True):
-    """(tensor, leading dimension) of a matrix, or of a vector (leading dimension 0)."""
+    """(address, leading dimension) of a matrix, or of a vector (leading dimension 0); (None, 0) of none."""
     if t is None:
         if not optional:
             raise ValueError(f"{name} is needed")
         return None, 0
-    ld = B.native.leading(t, shape, TORCH_TYPES.get(dtype), device)
-    if ld >= 0:
-        return t, ld
+    at = B.native.place(t, shape, TORCH_TYPES.get(dtype), device)
+    if at is not None:
+        return at
     # what is wrong with it
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} is not a tensor")
@@ -39,5 +39,5 @@ def own_device(device) -> torch.device:
 
 def check_device(device: torch.device) -> None:
     """Kernels are launched on the current device, and on its current stream where none is given."""
-    if device.type == "cuda" and B.current_device() != device.index:
+    if device.index is not None and device.index != B.current_device() and device.type == "cuda":
         raise ValueError(f"the current device is cuda:{B.current_device()}, the tensors are on {device}")
