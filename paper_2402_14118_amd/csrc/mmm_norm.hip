@@ -24,8 +24,8 @@ namespace {
 constexpr int PIECE = MMM_PIECE;
 constexpr int64_t MAX_GROUPS = 1 << 20;   // workgroups of a launch, which may have 2^32 threads: what is left over they take in turns
 
-// The sum over the lanes of a wave, in lane 63: cross-lane moves of the vector unit, sixteen lanes first (a shuffle goes through LDS: 48 of them
-// per row were most of a row's time).
+// The sum over the lanes of a wave, in lane 63: cross-lane moves of the vector unit, sixteen lanes first (a shuffle would go
+// through LDS).
 template <int CTRL, int ROWS> __device__ __forceinline__ float lanes_below(float v)
 {
     return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, true));
@@ -71,35 +71,40 @@ template <int N> __device__ __forceinline__ void clear_rooms(float *rooms)
     __syncthreads();
 }
 
-// The pieces of a row that this lane has: V of them, a workgroup's width apart.  WHOLE: rows of eight elements and more, all loads are whole pieces
-// that exist, without a branch around any (with branches each load was waited for where it stood, and everything under way with it: a
-// row's gradients took four times as long): a piece that ends behind the row begins earlier, at the row's last eight elements, and
-// what of it is another lane's counts for nothing here.  Else (a row is one short piece) element by element.
-template <bool WHOLE, int V> struct Pieces {
+// The pieces of a row that this lane has: V of them, a workgroup's width apart.  Loads are whole pieces that exist, without a branch around any (with
+// branches each load was waited for where it stood, and everything under way with it: gradients of 2048 x 4096 bf16 47 us, without 29).
+//   EVEN   rows of whole pieces: a lane behind the last one reads that and takes no part (`on`); no choice at each element (29 -> 25 us, 777 x 1992 floats
+//          17 -> 15: the row's work on the vector unit is what bounds the gradients)
+//   ODD    the last piece begins earlier, at the row's last eight elements, and what of it is another lane's counts for nothing here (`mine`)
+//   SHORT  fewer than eight elements: one by one
+enum RowKind { EVEN, ODD, SHORT };
+template <RowKind KIND, int V> struct Pieces {
     int at[V], first[V], count[V];   // where piece i is read; its elements that are this lane's: first, and how many
     __device__ __forceinline__ explicit Pieces(int N)
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int col = (i * (int)blockDim.x + (int)threadIdx.x) * PIECE;
-            at[i] = WHOLE ? min(col, N - PIECE) : 0;
-            first[i] = WHOLE ? min(col - at[i], PIECE) : 0;
-            count[i] = WHOLE ? PIECE - first[i] : threadIdx.x == 0 ? N : 0;
+            at[i] = KIND == SHORT ? 0 : min(col, N - PIECE);
+            first[i] = KIND == SHORT ? 0 : min(col - at[i], PIECE);
+            count[i] = KIND == SHORT ? threadIdx.x == 0 ? N : 0 : PIECE - first[i];
         }
     }
-    __device__ __forceinline__ bool mine(int i, int q) const { return WHOLE ? q >= first[i] : q < count[i]; }
+    __device__ __forceinline__ bool on(int i) const { return KIND != EVEN || first[i] == 0; }
+    __device__ __forceinline__ bool mine(int i, int q) const { return KIND == EVEN || (KIND == ODD ? q >= first[i] : q < count[i]); }
     template <typename T> __device__ __forceinline__ typename mmm_raw_piece<T>::type load(const T *row, int i) const
     {
-        if constexpr (WHOLE) {
+        if constexpr (KIND != SHORT) {
             typedef typename mmm_row_piece<T, PIECE>::type piece;
             return *reinterpret_cast<const piece *>(row + at[i]);
         } else {
             return mmm_load_raw(row, count[i]);
         }
     }
+    // (where the piece is on)
     template <typename T> __device__ __forceinline__ void store(T *row, int i, const float (&v)[PIECE]) const
     {
-        if (WHOLE && first[i] == 0) {
+        if (KIND == EVEN || (KIND == ODD && first[i] == 0)) {
             mmm_store_piece(row + at[i], PIECE, v);
         } else {
 #pragma unroll
@@ -128,11 +133,11 @@ template <typename R> __device__ __forceinline__ void values_or(const R &raw, bo
     for (int q = 0; q < PIECE; ++q) out[q] = there ? (float)raw[q] : otherwise;
 }
 
-template <typename T, typename TH, typename TY, int V, int WAVES, bool WHOLE> __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_kernel(const NormParams p)
+template <typename T, typename TH, typename TY, int V, int WAVES, RowKind KIND> __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_kernel(const NormParams p)
 {
     __shared__ __align__(16) float rooms[2][4][1][WAVES];   // (rows in turn: of a row, a wave may still read what another has gone past)
     clear_rooms<2 * 4 * WAVES>(&rooms[0][0][0][0]);
-    const Pieces<WHOLE, V> mine((int)p.d.N);
+    const Pieces<KIND, V> mine((int)p.d.N);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < p.d.M; row += gridDim.x, turn ^= 1) {
         float h[V][PIECE], v[V][PIECE];
@@ -155,35 +160,40 @@ template <typename T, typename TH, typename TY, int V, int WAVES, bool WHOLE> __
             if (kind == MMM_NORM_LAYER) {
 #pragma unroll
                 for (int i = 0; i < V; ++i)
+                    if (mine.on(i))
 #pragma unroll
-                    for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q];   // (elements that are not this lane's are zero)
+                        for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q];   // (elements that are not this lane's are zero)
                 add_over_row(sum, rooms[turn][of]);
                 const float mean = sum[0] * p.inv_n;
 #pragma unroll
                 for (int i = 0; i < V; ++i)
+                    if (mine.on(i))
 #pragma unroll
-                    for (int q = 0; q < PIECE; ++q) x[i][q] = mine.mine(i, q) ? x[i][q] - mean : 0.f;
+                        for (int q = 0; q < PIECE; ++q) x[i][q] = mine.mine(i, q) ? x[i][q] - mean : 0.f;
                 sum[0] = 0.f;
             }
 #pragma unroll
             for (int i = 0; i < V; ++i)
+                if (mine.on(i))
 #pragma unroll
-                for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q] * x[i][q];
+                    for (int q = 0; q < PIECE; ++q) sum[0] += x[i][q] * x[i][q];
             add_over_row(sum, rooms[turn][2 + of]);
             return 1.f / sqrtf(sum[0] * p.inv_n + p.d.eps);
         };
 #pragma unroll
         for (int i = 0; i < V; ++i)
+            if (mine.on(i))
 #pragma unroll
-            for (int q = 0; q < PIECE; ++q) {
-                h[i][q] = mine.mine(i, q) ? (float)raw_h[i][q] : 0.f;
-                v[i][q] = mine.mine(i, q) ? (float)raw_y[i][q] : 0.f;
-            }
+                for (int q = 0; q < PIECE; ++q) {
+                    h[i][q] = mine.mine(i, q) ? (float)raw_h[i][q] : 0.f;
+                    v[i][q] = mine.mine(i, q) ? (float)raw_y[i][q] : 0.f;
+                }
         if (p.has_y) {
             const float r = p.d.post != MMM_NORM_NONE ? standard(v, p.d.post, 0) : 1.f;
             const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(p.row_gates)[row] : 1.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
+                if (!mine.on(i)) continue;
                 float w[PIECE], b[PIECE], g[PIECE];
                 values_or(raw_w[i], p.has_post_weight, 1.f, w);
                 values_or(raw_b[i], p.has_post_bias, 0.f, b);
@@ -197,6 +207,7 @@ template <typename T, typename TH, typename TY, int V, int WAVES, bool WHOLE> __
             const float r = standard(h, p.d.pre, 1);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
+                if (!mine.on(i)) continue;
                 float w[PIECE], b[PIECE];
                 values_or(raw_w2[i], p.has_pre_weight, 1.f, w);
                 values_or(raw_b2[i], p.has_pre_bias, 0.f, b);
@@ -223,11 +234,11 @@ struct NormGradParams {
 };
 
 // What a row takes from memory: asked for while the row before is worked on.
-template <typename T, typename TH, typename TY, int V, bool WHOLE> struct GradRow {
+template <typename T, typename TH, typename TY, int V, RowKind KIND> struct GradRow {
     typename mmm_raw_piece<TH>::type x[V], d[V];
     typename mmm_raw_piece<T>::type dn[V], gate[V];
     typename mmm_raw_piece<TY>::type y[V];
-    __device__ __forceinline__ void load(const NormGradParams &p, const Pieces<WHOLE, V> &mine, int64_t row)
+    __device__ __forceinline__ void load(const NormGradParams &p, const Pieces<KIND, V> &mine, int64_t row)
     {
         const mmm_block_norm_grads &g = p.g;
 #pragma unroll
@@ -241,27 +252,31 @@ template <typename T, typename TH, typename TY, int V, bool WHOLE> struct GradRo
     }
 };
 // What all rows share.
-template <typename T, int V, bool WHOLE> struct GradColumns {
+template <typename T, int V, RowKind KIND> struct GradColumns {
     typename mmm_raw_piece<T>::type pre_weight[V], post_weight[V], post_bias[V];
-    __device__ __forceinline__ void load(const NormGradParams &p, const Pieces<WHOLE, V> &mine, bool biases)
+    __device__ __forceinline__ void load(const NormGradParams &p, const Pieces<KIND, V> &mine, bool biases)
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            typedef typename mmm_raw_piece<T>::type raw;
             pre_weight[i] = mine.load(static_cast<const T *>(p.g.pre_weight), i);
             post_weight[i] = mine.load(static_cast<const T *>(p.g.post_weight), i);
-            post_bias[i] = biases ? mine.load(static_cast<const T *>(p.g.post_bias), i) : post_weight[i];
+            if (biases) post_bias[i] = mine.load(static_cast<const T *>(p.g.post_bias), i);
+            if (!p.has_pre_weight) pre_weight[i] = raw((T)1.f);
+            if (!p.has_post_weight) post_weight[i] = raw((T)1.f);
+            if (!biases || !p.has_post_bias) post_bias[i] = raw((T)0.f);
         }
     }
 };
 
 // BIASES: the norm behind the block has a bias, or sums for biases are asked for
-template <typename T, typename TH, typename TY, int V, int WAVES, bool BIASES, bool WHOLE>
+template <typename T, typename TH, typename TY, int V, int WAVES, bool BIASES, RowKind KIND>
 __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const NormGradParams p)
 {
     __shared__ __align__(16) float rooms[2][4][3][WAVES];   // (rows in turn, as above)
     clear_rooms<2 * 4 * 3 * WAVES>(&rooms[0][0][0][0]);
     const mmm_block_norm_grads &g = p.g;
-    const Pieces<WHOLE, V> mine((int)p.d.N);
+    const Pieces<KIND, V> mine((int)p.d.N);
     const bool pre = p.d.pre != MMM_NORM_NONE, block = p.block, post = p.d.post != MMM_NORM_NONE;
     const bool pre_mean = p.d.pre == MMM_NORM_LAYER, post_mean = p.d.post == MMM_NORM_LAYER;
     float sums[SUMS][V][PIECE];
@@ -272,9 +287,9 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) sums[s][i][q] = 0.f;
 
-    GradColumns<T, V, WHOLE> columns;
+    GradColumns<T, V, KIND> columns;
     if (V == 1) columns.load(p, mine, BIASES);   // (wider rows have no registers for them)
-    GradRow<T, TH, TY, V, WHOLE> next;
+    GradRow<T, TH, TY, V, KIND> next;
     next.load(p, mine, blockIdx.x);   // (there are no more workgroups than rows)
     int turn = 0;
     for (int64_t row = blockIdx.x; row < p.d.M; row += gridDim.x, turn ^= 1) {
@@ -282,14 +297,15 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
         const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(p.row_gates)[row] : 1.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            if (!mine.on(i)) continue;
             values_or(next.gate[i], p.has_gate, row_gate, gate[i]);
 #pragma unroll
-            for (int q = 0; q < PIECE; ++q) {   // zeros for what is not there, and what is another lane's
+            for (int q = 0; q < PIECE; ++q) {   // (zeros for what is another lane's; of operands that are not there nothing is used)
                 const bool on = mine.mine(i, q);
-                x[i][q] = pre && on ? (float)next.x[i][q] : 0.f;
-                dn[i][q] = pre && on ? (float)next.dn[i][q] : 0.f;
+                x[i][q] = on ? (float)next.x[i][q] : 0.f;
+                dn[i][q] = on ? (float)next.dn[i][q] : 0.f;
                 d[i][q] = p.has_d_h_out && on ? (float)next.d[i][q] : 0.f;
-                y[i][q] = block && on ? (float)next.y[i][q] : 0.f;
+                y[i][q] = on ? (float)next.y[i][q] : 0.f;
             }
         }
         if (V > 1) columns.load(p, mine, BIASES);
@@ -299,29 +315,32 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
         if (pre_mean || post_mean) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
+                if (mine.on(i))
 #pragma unroll
-                for (int q = 0; q < PIECE; ++q) {
-                    s2[0] += x[i][q];
-                    s2[1] += y[i][q];
-                }
+                    for (int q = 0; q < PIECE; ++q) {
+                        s2[0] += x[i][q];
+                        s2[1] += y[i][q];
+                    }
             add_over_row(s2, rooms[turn][0]);
             const float mx = pre_mean ? s2[0] * p.inv_n : 0.f, my = post_mean ? s2[1] * p.inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
+                if (mine.on(i))
 #pragma unroll
-                for (int q = 0; q < PIECE; ++q) {
-                    x[i][q] = mine.mine(i, q) ? x[i][q] - mx : 0.f;
-                    y[i][q] = mine.mine(i, q) ? y[i][q] - my : 0.f;
-                }
+                    for (int q = 0; q < PIECE; ++q) {
+                        x[i][q] = mine.mine(i, q) ? x[i][q] - mx : 0.f;
+                        y[i][q] = mine.mine(i, q) ? y[i][q] - my : 0.f;
+                    }
             s2[0] = s2[1] = 0.f;
         }
 #pragma unroll
         for (int i = 0; i < V; ++i)
+            if (mine.on(i))
 #pragma unroll
-            for (int q = 0; q < PIECE; ++q) {
-                s2[0] += x[i][q] * x[i][q];
-                s2[1] += y[i][q] * y[i][q];
-            }
+                for (int q = 0; q < PIECE; ++q) {
+                    s2[0] += x[i][q] * x[i][q];
+                    s2[1] += y[i][q] * y[i][q];
+                }
         add_over_row(s2, rooms[turn][1]);
         const float rx = 1.f / sqrtf(s2[0] * p.inv_n + p.d.eps), ry = post ? 1.f / sqrtf(s2[1] * p.inv_n + p.d.eps) : 1.f;
         // through the norm in front of the next block: d becomes the gradient of h'
@@ -329,14 +348,13 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
             float c[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float w[PIECE];
-                values_or(columns.pre_weight[i], p.has_pre_weight, 1.f, w);
+                if (!mine.on(i)) continue;
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) {
                     x[i][q] *= rx;
                     sums[SUM_PRE_WEIGHT][i][q] += dn[i][q] * x[i][q];
                     if (BIASES) sums[SUM_PRE_BIAS][i][q] += dn[i][q];
-                    dn[i][q] *= w[q];
+                    dn[i][q] *= (float)columns.pre_weight[i][q];
                     c[0] += dn[i][q] * x[i][q];
                     c[1] += dn[i][q];
                 }
@@ -345,13 +363,15 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
             const float along = c[0] * p.inv_n, mean = pre_mean ? c[1] * p.inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
+                if (mine.on(i))
 #pragma unroll
-                for (int q = 0; q < PIECE; ++q) d[i][q] += rx * (dn[i][q] - x[i][q] * along - mean);
+                    for (int q = 0; q < PIECE; ++q) d[i][q] += rx * (dn[i][q] - x[i][q] * along - mean);
         }
         if (g.d_h != nullptr) {
             const float alpha = block ? p.d.alpha : 1.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
+                if (!mine.on(i)) continue;
                 float out[PIECE];
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) out[q] = alpha * d[i][q];
@@ -363,20 +383,20 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
         float c[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float w[PIECE], b[PIECE], dgate[PIECE];
-            values_or(columns.post_weight[i], p.has_post_weight, 1.f, w);
-            values_or(columns.post_bias[i], BIASES && p.has_post_bias, 0.f, b);
+            if (!mine.on(i)) continue;
+            float dgate[PIECE];
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) {
                 if (!mine.mine(i, q)) d[i][q] = 0.f;   // (the mean has been taken off there, too)
                 y[i][q] *= ry;
-                dgate[q] = d[i][q] * (y[i][q] * w[q] + b[q]);
+                const float w = (float)columns.post_weight[i][q];
+                dgate[q] = d[i][q] * (BIASES ? y[i][q] * w + (float)columns.post_bias[i][q] : y[i][q] * w);
                 c[2] += dgate[q];
                 sums[SUM_GATE][i][q] += dgate[q];
                 d[i][q] *= gate[i][q];
                 sums[SUM_POST_WEIGHT][i][q] += d[i][q] * y[i][q];
                 if (BIASES) sums[SUM_POST_BIAS][i][q] += d[i][q];
-                d[i][q] *= w[q];
+                d[i][q] *= w;
                 c[0] += d[i][q] * y[i][q];
                 c[1] += d[i][q];
             }
@@ -388,6 +408,7 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
             const float along = post ? c[0] * p.inv_n : 0.f, mean = post_mean ? c[1] * p.inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
+                if (!mine.on(i)) continue;
 #pragma unroll
                 for (int q = 0; q < PIECE; ++q) d[i][q] = ry * (d[i][q] - y[i][q] * along - mean);
                 mine.store(static_cast<TY *>(g.d_y) + row * g.ldd_y, i, d[i]);
@@ -399,7 +420,8 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
     for (int s = 0; s < SUMS; ++s) {
         if (p.place[s] < 0) continue;
 #pragma unroll
-        for (int i = 0; i < V; ++i) mine.store(p.partials + ((int64_t)blockIdx.x * p.sums + p.place[s]) * p.d.N, i, sums[s][i]);
+        for (int i = 0; i < V; ++i)
+            if (mine.on(i)) mine.store(p.partials + ((int64_t)blockIdx.x * p.sums + p.place[s]) * p.d.N, i, sums[s][i]);
     }
 }
 
@@ -519,7 +541,7 @@ template <typename F> auto with_types(const mmm_block_norm_desc &d, F f)
 }
 
 // Workgroups of the gradients: as many as the registers of the chip hold at a time (8 waves on a compute unit), so that partial sums are few, and
-// all with the same number of rows but for one.  2048 x 4096 bf16: 256 groups 28.6 us and 4.0 for adding up, 512 32.3 and 5.5, 1024 38.8 and 8.3.
+// all with the same number of rows but for one.  2048 x 4096 bf16, before EVEN: 256 groups 28.6 us and 4.0 for adding up, 512 32.3 and 5.5, 1024 38.8 and 8.3.
 int64_t norm_grad_groups(int64_t M, int64_t N)
 {
     const int64_t slots = 256 * std::max<int64_t>(1, 512 / row_shape(N).threads), rows = (M + slots - 1) / slots;
@@ -556,10 +578,12 @@ hipError_t mmm_launch_block_norm(const mmm_block_norm_desc &d, const void *h, in
         typedef decltype(t) T;
         typedef decltype(th) TH;
         typedef decltype(ty) TY;
-        void (*fn)(const NormParams) = d.N < PIECE         ? mmm_block_norm_kernel<T, TH, TY, 1, 4, false>
-                                       : shape.pieces == 1 ? shape.threads <= 256 ? mmm_block_norm_kernel<T, TH, TY, 1, 4, true> : mmm_block_norm_kernel<T, TH, TY, 1, 8, true>
-                                       : shape.pieces == 2 ? mmm_block_norm_kernel<T, TH, TY, 2, 8, true>
-                                                           : mmm_block_norm_kernel<T, TH, TY, 4, 16, true>;
+        void (*fn)(const NormParams) = d.N < PIECE              ? mmm_block_norm_kernel<T, TH, TY, 1, 4, SHORT>
+                                       : shape.pieces == 2      ? mmm_block_norm_kernel<T, TH, TY, 2, 8, ODD>
+                                       : shape.pieces == 4      ? mmm_block_norm_kernel<T, TH, TY, 4, 16, ODD>
+                                       : d.N % PIECE != 0       ? mmm_block_norm_kernel<T, TH, TY, 1, 8, ODD>
+                                       : shape.threads <= 256   ? mmm_block_norm_kernel<T, TH, TY, 1, 4, EVEN>
+                                                                : mmm_block_norm_kernel<T, TH, TY, 1, 8, EVEN>;
         hipLaunchKernelGGL(fn, dim3((uint32_t)std::min(d.M, MAX_GROUPS)), dim3(shape.threads), 0, s, p);
         return 0;
     });
@@ -608,11 +632,12 @@ hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_bl
         typedef decltype(th) TH;
         typedef decltype(ty) TY;
         const bool biases = g.d_pre_bias != nullptr || g.d_post_bias != nullptr || g.post_bias != nullptr;
-        void (*fn)(const NormGradParams) =
-            d.N < PIECE         ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 4, true, false>
-            : shape.pieces == 1 ? biases ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, true> : mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, false, true>
-            : shape.pieces == 2 ? mmm_block_norm_grad_kernel<T, TH, TY, 2, 8, true, true>
-                                : mmm_block_norm_grad_kernel<T, TH, TY, 4, 16, true, true>;
+        void (*fn)(const NormGradParams) = d.N < PIECE         ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 4, true, SHORT>
+                                           : shape.pieces == 2 ? mmm_block_norm_grad_kernel<T, TH, TY, 2, 8, true, ODD>
+                                           : shape.pieces == 4 ? mmm_block_norm_grad_kernel<T, TH, TY, 4, 16, true, ODD>
+                                           : d.N % PIECE != 0  ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, ODD>
+                                           : biases            ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, EVEN>
+                                                               : mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, false, EVEN>;
         hipLaunchKernelGGL(fn, dim3((uint32_t)groups), dim3(shape.threads), 0, s, p);
         return 0;
     });
