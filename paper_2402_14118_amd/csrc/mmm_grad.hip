@@ -470,7 +470,9 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
     if (m->b_compact && (dX != nullptr || clear_y)) {
         const ClearParams c{static_cast<char *>(dX), clear_y ? reinterpret_cast<char *>(dY) : nullptr, lddx * esz, m->K * esz, m->M, lddy * 4, m->N * 4, m->K, m->rows_copy};
         const int64_t bytes = std::max(dX != nullptr ? c.dx_bytes : 0, clear_y ? c.dy_bytes : 0), rows = std::max(dX != nullptr ? c.M : 0, clear_y ? c.K : 0);
-        const dim3 grid((uint32_t)std::min<int64_t>((bytes + 4095) / 4096, 16), (uint32_t)std::min<int64_t>(rows, 8192), dX != nullptr && clear_y ? 2 : 1);
+        // some 2048 workgroups that go from row to row (one for each row: 11.4 us for 777 x 3001 and 3001 x 1992 floats, so 7.8)
+        const uint32_t across = (uint32_t)std::min<int64_t>((bytes + 4095) / 4096, 16), both = dX != nullptr && clear_y ? 2 : 1;
+        const dim3 grid(across, (uint32_t)std::min<int64_t>(rows, 2048 / (across * both)), both);
         hipLaunchKernelGGL(mmm_grad_clear_kernel, grid, dim3(256), 0, s, c);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
