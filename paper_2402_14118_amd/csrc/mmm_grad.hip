@@ -2,8 +2,8 @@
 //     dX[i,k] = a_bits[i,k] ? sum over j of dC[i,j] B[k,j] : 0         B = N(Y), A = M(X)
 //     dY[k,j] = b_bits[k,jb] ? sum over i of A[i,k] dC[i,j] : 0
 // Both on matrix instructions, over all k, or in row-compacted mode over the live rows k' alone, whose number and places the maps hold.
-// Zeros of A inside a tile and blocks of B that are off are multiplied as zeros (their elements are not random here: A's zeros decide which of the
-// results are wanted, 64 x 128 of which share a tile); what is not wanted is dropped at the end.
+// Zeros of A and blocks of B that are off are multiplied as zeros, and results that are not wanted are worked out and dropped: of a tile of random elements
+// of A, or of 64 rows with random blocks, nearly all are wanted somewhere.
 //
 // One kernel for both: a workgroup owns a tile of `TR` x `TL` results and walks the contraction in steps of 128 bytes (64 elements of the 16-bit types, 32
 // floats).  R is the operand along which a lane holds four neighbouring results, so that they are stored together; L the other.
@@ -12,9 +12,14 @@
 //     dY        columns of dC, j           columns of A, k            contraction i
 // A comes from the image that the builder made, masked, compacted and with 16 (floats: 4) rows of a column side by side, which is the
 // order that an operand of dY wants.  dC is read row by row there, and turned by ds_read_b64_tr_b16 (floats: one by one) on the way out of LDS.
-// Operands wait in registers while the step before is multiplied, and are laid into the other half of LDS behind it: masks are applied on the
-// way, one barrier per step.  In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that
+// Operands wait in registers while the step before is multiplied, and are laid into the other half of LDS between its last products: masks are applied on the
+// way, one barrier per step (placed behind the products instead: 2048 x 16384 x 4096 bf16, both gradients, 612 us for 565).  In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that
 // eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
+//
+// What bounds it.  Large results: the matrix cores at the clock that the power limit leaves (4096^3 half 1096 TFLOP/s for both, where a library product
+// of 8192^3 bf16 reaches 1140; 2048 x 16384 x 4096 bf16 973; floats 135 of 155).  Small ones: the steps of a workgroup, one after another, and two to five
+// launches.  Rows by context: the zeros of dX and of the rows of dY that are off (2048 x 16384 x 4096 bf16, a tenth of the rows: 190 us, 335 MB of results).
+// Operands of the smallest tile two steps ahead, in registers: no faster.
 #include <algorithm>
 #include <type_traits>
 
