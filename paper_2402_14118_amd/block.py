@@ -111,8 +111,6 @@ class MaskedMlp:
         self.up = MaskedMatmul(M, width, hidden, block_width, dtype, self.device)
         self.down = MaskedMatmul(M, hidden, width, block_width, dtype, self.device)
         self.norm = BlockNorm(M, width, dtype, post, pre, gate, alpha, eps, dtype_h, training=training, device=self.device)
-        # zeros of ReLU are told by the sign, those of a smooth activation by the value
-        self.pred = B.MMM_PRED_GT if activation == B.MMM_ACT_RELU else B.MMM_PRED_NONZERO
         self.up.set_path(B.MMM_PATH_MATRIX)
         if activation != B.MMM_ACT_RELU:
             self.down.set_path(B.MMM_PATH_MATRIX)
@@ -159,8 +157,8 @@ class MaskedMlp:
         self.up.build_maps(N, None, stream=stream)
         self.up.matmul_epilogue(N, self.W1, self.a, bias=self.b1, activation=self.activation, preact=kept, stream=stream)
         if not self.fused:
-            self.down.build_maps(self.a, None, self.pred, stream=stream)
-        self.down.matmul_epilogue(self.a, self.W2, self.y, bias=self.b2, pred=self.pred if self.fused else None, stream=stream)
+            self.down.build_maps(self.a, None, stream=stream)   # (by the value, not by the sign: NaN has to reach the stream)
+        self.down.matmul_epilogue(self.a, self.W2, self.y, bias=self.b2, pred=B.MMM_PRED_NONZERO if self.fused else None, stream=stream)
         self.norm.forward(H, normed=normed, H_out=H_out, Y=self.y, gate=gate, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight,
                           pre_bias=pre_bias, stream=stream)
 

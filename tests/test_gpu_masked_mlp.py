@@ -135,3 +135,40 @@ def test_counted():
     mlp.count()
     mlp.forward(d["N"], d["H"], second, n, **values)
     close(second, first.double().cpu(), "f32", "H_out")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,fused", [(5, True), (5, False), (40, False)])
+def test_nan_reaches_the_stream(M, fused):
+    """A row that is not a number stays one behind ReLU and its mask, and touches no other."""
+    mlp, d, *_ = setup("bf16", "relu", M=M, context=False, fused=fused)
+    values = {k: d[k] for k in ("gate", "post_weight", "pre_weight", "pre_bias")}
+    want, got, n = torch.empty_like(d["H"]), torch.empty_like(d["H"]), torch.empty_like(d["H"])
+    mlp.forward(d["N"], d["H"], want, n, **values)
+    assert bool(want.isfinite().all())
+    d["N"][3, 7] = float("nan")
+    mlp.forward(d["N"], d["H"], got, n, **values)
+    others = [i for i in range(M) if i != 3]
+    assert bool(got[3].isnan().all()) and bool(n[3].isnan().all()) and torch.equal(got[others], want[others])
+
+
+@pytest.mark.gpu
+def test_two_blocks_at_once():
+    """A holder each, on streams of their own, give what they give one after the other."""
+    blocks = [setup(dt, act, M=300, d=256, f=512, context=False)[:2] for dt, act in (("bf16", "relu"), ("f32", "silu"))]
+    wants, gots, streams = [], [], [torch.cuda.Stream() for _ in blocks]
+
+    def call(mlp, d, out):
+        mlp.forward(d["N"], d["H"], *out, **{k: d[k] for k in ("gate", "post_weight", "pre_weight", "pre_bias")})
+    for mlp, d in blocks:
+        wants.append((torch.empty_like(d["H"]), torch.empty_like(d["H"])))
+        gots.append([(torch.zeros_like(d["H"]), torch.zeros_like(d["H"])) for _ in range(4)])
+        call(mlp, d, wants[-1])
+    torch.cuda.synchronize()
+    for i in range(4):
+        for (mlp, d), out, s in zip(blocks, gots, streams):
+            with torch.cuda.stream(s):
+                call(mlp, d, out[i])
+    torch.cuda.synchronize()
+    for want, out in zip(wants, gots):
+        assert all(torch.equal(a, b) for pair in out for a, b in zip(want, pair))
