@@ -984,6 +984,8 @@ mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype o
     if (mmm_status st = mmm_epilogue_backward_workspace_bytes(M, N, &need); st != MMM_OK) return st;
     if (mmm_status st = planes_ok({{dC, lddc, out_dtype}, {activation != MMM_ACT_NONE ? Z : nullptr, ldz, out_dtype}, {dZ, lddz, dt}, {dbias, N, MMM_F32}}, N); st != MMM_OK)
         return st;
+    if (dZ != nullptr && ((dZ == dC && lddz != lddc) || (dZ == Z && lddz != ldz))) return MMM_ERR_SHAPE;
+    if (dZ != nullptr && (dZ == dC || dZ == Z) && dt != out_dtype) return MMM_ERR_DTYPE;
     if (dbias != nullptr && !workspace_ok(workspace, workspace_bytes, need)) return MMM_ERR_WORKSPACE;
     if (hipError_t e = mmm_launch_epilogue_grad(M, N, dt, out_dtype, activation, dC, lddc, Z, ldz, dZ, lddz, dbias, workspace, static_cast<hipStream_t>(hip_stream));
         e != hipSuccess) {

@@ -91,6 +91,14 @@ def test_epilogue_backward_refuses():
     assert B.lib.mmm_epilogue_backward_workspace_bytes(1, 1, None) == B.MMM_ERR_INVALID_ARG
 
 
+def test_epilogue_backward_in_place_is_in_place():
+    """dZ at the address of dC or Z, with rows or elements of another size."""
+    def call(dZ, lddz, dt=1, act=1, lddc=16, ldz=16):
+        return B.lib.mmm_epilogue_backward(4, 16, dt, 0, act, at(0), lddc, at(1), ldz, dZ, lddz, None, None, 0, None)
+    assert call(at(0), 17, dt=0) == call(at(1), 17, dt=0) == call(at(1), 16, dt=0, ldz=17) == B.MMM_ERR_SHAPE
+    assert call(at(0), 16) == call(at(1), 16) == B.MMM_ERR_DTYPE
+
+
 def test_the_holder_checks_tensors():
     norm = mm.BlockNorm(4, 16, mm.MMM_BF16, post=mm.MMM_NORM_RMS, gate=mm.MMM_GATE_ROW, device="cpu")
     H = torch.zeros(4, 16, dtype=torch.bfloat16)
