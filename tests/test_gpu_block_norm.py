@@ -370,3 +370,27 @@ def test_slopes_at_the_ends(act):
     assert got[2] == got[4] == got[6] == 2.0 and got[3] == got[5] == got[7] == low
     assert abs(got[8] - 2.0) < 1e-6 and abs(got[9] - low) < 1e-6
     assert act == "none" or math.isnan(got[11])
+
+
+@pytest.mark.gpu
+def test_more_elements_than_32_bits_count():
+    """The last rows of matrices of more than 2^32 elements come out as those of a matrix of their own; sums of whole numbers are exact."""
+    M, N, tail = 131100, 32768, 64
+    g = torch.Generator().manual_seed(2)
+    ends = [torch.randint(-3, 4, (tail, N), generator=g).bfloat16().cuda() for _ in range(3)]
+    whole = [torch.ones(M, N, dtype=torch.bfloat16, device="cuda") for _ in ends]
+    for w, e in zip(whole, ends):
+        w[-tail:] = e
+    (H, Y, D), out, results = whole, torch.empty_like(whole[0]), []
+    for rows, (h, y, d, to) in ((tail, (*ends, torch.empty_like(ends[0]))), (M, (H, Y, D, out))):
+        norm = mm.BlockNorm(rows, N, mm.MMM_BF16, post=mm.MMM_NORM_RMS, training=True)
+        norm.forward(h, normed=to, H_out=h, Y=y)          # (in place)
+        parts = [h[-tail:].clone(), to[-tail:].clone()]
+        norm.backward(H_out=h, grad_normed=d, grad_H=to, Y=y)
+        parts.append(to[-tail:].clone())
+        dbias = torch.empty(N, device="cuda")
+        ws = torch.empty(mm.mmm_epilogue_backward_workspace_bytes(rows, N), dtype=torch.uint8, device="cuda")
+        mm.binding.mmm_epilogue_backward(rows, N, mm.MMM_BF16, mm.MMM_BF16, mm.MMM_ACT_RELU, y, N, y, N, to, N, dbias, ws, ws.numel())
+        assert torch.equal(dbias, ends[1].float().clamp(min=0).sum(0) + (rows - tail))
+        results.append(parts + [to[-tail:].clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))

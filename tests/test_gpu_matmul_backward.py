@@ -187,3 +187,60 @@ def test_tiles_and_parts(dt, M, K, N, rows):
         more = dY.clone()
         eng.matmul_backward(X, Y, dC, dY=more, accumulate=True)
         assert torch.equal(more, dY + dY)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_a_captured_step_with_another_selection(dt):
+    """The maps are made again inside a graph: replays follow the rows selected then, of which there may be far more than when it was captured."""
+    M, K, N = 200, 3000, 264
+    g = torch.Generator().manual_seed(5)
+    t = T[dt][1]
+    X, Y, dC = (torch.randn(s, generator=g).to(t).cuda() for s in ((M, K), (K, N), (M, N)))
+    few, many = (words(torch.rand(1, K, generator=g) < p) for p in (0.02, 0.95))
+    chosen = few.clone()
+    eng = mm.MaskedMatmul(M, K, N, 8, T[dt][0])
+    dX, dY = torch.empty_like(X), torch.empty(K, N, device="cuda")
+
+    def call():
+        eng.build_maps(X, Y, keep_rows=chosen)
+        eng.matmul_backward(X, Y, dC, dX, dY)
+    call()
+    eng.stats()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for rows in (many, few, many, torch.zeros_like(few)):
+        chosen.copy_(rows)
+        dX.fill_(3.0)
+        dY.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        bits = (rows.view(torch.uint8).cpu().view(-1, 1) >> torch.arange(8, dtype=torch.uint8) & 1).reshape(-1)[:K].bool().cuda()
+        B, A, G = Y.double() * bits.view(-1, 1), X.double(), dC.double()
+        a_on = (X != 0)
+        want, mag = (G @ B.t().contiguous()) * a_on, G.abs() @ B.abs().t().contiguous()
+        assert bool(((dX.double() - want).abs() <= (N + 1) * U * mag + torch.finfo(t).eps / 2 * want.abs() * (1 + 1e-3)).all())
+        want, mag = (A.t().contiguous() @ G) * bits.view(-1, 1), A.abs().t().contiguous() @ G.abs()
+        assert bool(((dY.double() - want).abs() <= (M + 1) * U * mag).all())
+
+
+@pytest.mark.gpu
+def test_rows_far_apart():
+    """Leading dimensions next to the largest: offsets of rows pass 32 bits."""
+    M, K, N, ld = 1100, 1030, 64, (1 << 22) - 8
+    g = torch.Generator().manual_seed(9)
+    host = [torch.randn(s, generator=g).bfloat16() for s in ((M, K), (K, N), (M, N))]
+    near = [v.cuda() for v in host]
+    far = [torch.empty(v.shape[0] * ld, dtype=v.dtype, device="cuda").as_strided(v.shape, (ld, 1)).copy_(v) for v in near]
+    results = []
+    for (X, Y, dC), pitch in ((near, None), (far, ld)):
+        eng = mm.MaskedMatmul(M, K, N, 8, mm.MMM_BF16)
+        eng.build_maps(X, Y)
+        room = lambda v, t: torch.empty(v.shape, dtype=t, device="cuda") if pitch is None else torch.empty(v.shape[0] * pitch, dtype=t, device="cuda").as_strided(v.shape, (pitch, 1))
+        dX, dY, C = room(X, X.dtype), room(Y, torch.float32), room(dC, dC.dtype)
+        eng.matmul_backward(X, Y, dC, dX, dY)
+        eng.matmul_epilogue(X, Y, C, activation=mm.MMM_ACT_SILU, residual=dC)
+        results.append([v.clone(memory_format=torch.contiguous_format) for v in (dX, dY, C)])
+        eng.close()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
