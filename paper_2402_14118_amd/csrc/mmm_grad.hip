@@ -17,8 +17,8 @@
 // eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
 //
 // What bounds it.  Large results: the matrix cores at the clock that the power limit leaves (4096^3 half 1096 TFLOP/s for both, where a library product
-// of 8192^3 bf16 reaches 1140; 2048 x 16384 x 4096 bf16 973; floats 135 of 155).  Small ones: the steps of a workgroup, one after another, and two to five
-// launches.  Rows by context: the zeros of dX and of the rows of dY that are off (2048 x 16384 x 4096 bf16, a tenth of the rows: 190 us, 335 MB of results).
+// of 8192^3 bf16 reaches 1140; 2048 x 16384 x 4096 bf16 973; floats 135 of 155).  Small ones: the steps of a workgroup, one after another, and one to four
+// launches.  Rows by context: the zeros of dX and of the rows of dY that are off (2048 x 16384 x 4096 bf16, a tenth of the rows: 214 us, 335 MB of results).
 // Operands of the smallest tile two steps ahead, in registers: no faster.
 #include <algorithm>
 #include <type_traits>
@@ -76,12 +76,12 @@ template <typename T, bool TO_X> __device__ __forceinline__ void store_results(c
                 for (int u = 0; u < 4; ++u)
                     if (r + u < live) row[r + u] = to[u];
             }
-        } else {   // (the row holds zeros)
+        } else {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 if (r + u >= live) continue;
                 const uint32_t k = p.kmap[r + u];
-                if (bits == nullptr || (bits[k >> 6] >> (k & 63u) & 1ull)) row[k] = (T)v[u];
+                row[k] = bits == nullptr || (bits[k >> 6] >> (k & 63u) & 1ull) ? (T)v[u] : (T)0.f;
             }
         }
     } else {
@@ -110,9 +110,9 @@ template <typename T> __device__ __forceinline__ void multiply(const u32x4 &r, c
     }
 }
 
-// T: float, _Float16 or __bf16.  WR x WL waves, each FR x FL tiles of 16 x 16.
+// One gradient: workgroup `group` of those that it has.  T: float, _Float16 or __bf16.  WR x WL waves, each FR x FL tiles of 16 x 16.
 template <typename T, bool TO_X, int WR, int WL, int FR, int FL>
-__global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradParams p)
+__device__ __forceinline__ void gradient(const GradParams &p, uint32_t group, char (&lds)[2][256 * (FL * WL + FR * WR) * 8])
 {
     constexpr int ESZ = (int)sizeof(T), NT = 64 * WR * WL, TR = 16 * FR * WR, TL = 16 * FL * WL;
     constexpr int STEP = ROWB / ESZ, PER = 16 / ESZ;          // elements of the contraction per step, and of a piece
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
     constexpr uint32_t TURN = TR / 16 < 8 ? TR / 16 - 1 : 7;  // and which of its sixteen columns take each other's place
     constexpr uint32_t OUTSIDE = 0x80000000u;                 // past the end of the buffers below, whatever else is added
     static_assert(NL * NT == TL * 8 && NR * NT == TR * 8, "whole pieces");
-    __shared__ __align__(16) char lds[2][(TL + TR) * ROWB];
+    static_assert(sizeof(lds) == 2 * (TL + TR) * ROWB, "two steps");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, s = lane >> 4, wr = wave % WR, wl = wave / WR;
@@ -131,8 +131,8 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
     const uint32_t size_r = TO_X ? live : (uint32_t)p.N, size_l = TO_X ? (uint32_t)p.M : live;
     const uint32_t tiles_r = (size_r + TR - 1) / TR, tiles_l = (size_l + TL - 1) / TL, tiles = tiles_r * tiles_l;
     const uint32_t all = tiles * (uint32_t)p.splits;
-    if (blockIdx.x >= all) return;
-    const uint32_t q8 = all >> 3, rem = all & 7u, x = blockIdx.x & 7u, id = x * q8 + min(x, rem) + (blockIdx.x >> 3);
+    if (group >= all) return;
+    const uint32_t q8 = all >> 3, rem = all & 7u, x = group & 7u, id = x * q8 + min(x, rem) + (group >> 3);
     const uint32_t split = id / tiles, t = id - split * tiles;
     const uint32_t panel = t / (8 * tiles_l), width = min(8u, tiles_r - panel * 8), in_panel = t - panel * 8 * tiles_l;
     const uint32_t r0 = (panel * 8 + in_panel % width) * TR, l0 = in_panel / width * TL;
@@ -336,8 +336,65 @@ __global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradPar
     }
 }
 
+// Row-compacted mode: zeros where no tile writes, the columns of dX and the rows of dY that are off.
+struct ClearParams {
+    char *dX, *dY;   // null: not asked for
+    int64_t dx_pitch, M, dy_pitch, dy_bytes, K;
+    const uint64_t *rows;
+    uint32_t groups;
+};
+template <int ESZ> __device__ __forceinline__ void clear(const ClearParams &p, uint32_t group)
+{
+    typedef typename AnyPiece<ESZ>::type piece_any;
+    typedef std::conditional_t<ESZ == 4, uint32_t, uint16_t> bits_t;
+    typedef bits_t element __attribute__((may_alias));
+    constexpr int PER = 16 / ESZ;
+    const int64_t rows_x = p.dX != nullptr ? p.M : 0, rows_y = p.dY != nullptr ? p.K : 0;
+    for (int64_t row = group; row < rows_x + rows_y; row += p.groups) {
+        if (row < rows_x) {
+            char *const out = p.dX + row * p.dx_pitch;
+            for (int64_t k = (int64_t)threadIdx.x * PER; k < p.K; k += (int64_t)blockDim.x * PER) {
+                const uint32_t live = (uint32_t)(p.rows[k >> 6] >> (k & 63)) & ((1u << PER) - 1u);
+                if (live == 0 && k + PER <= p.K) {
+                    *reinterpret_cast<piece_any *>(out + k * ESZ) = piece_any{0, 0, 0, 0};
+                } else {
+#pragma unroll
+                    for (int q = 0; q < PER; ++q)
+                        if (k + q < p.K && !(live >> q & 1u)) *reinterpret_cast<element *>(out + (k + q) * ESZ) = 0;
+                }
+            }
+        } else {
+            const int64_t k = row - rows_x;
+            if (p.rows[k >> 6] >> (k & 63) & 1ull) continue;
+            typedef AnyPiece<4>::type floats_any;
+            for (int64_t at = (int64_t)threadIdx.x * 16; at < p.dy_bytes; at += (int64_t)blockDim.x * 16)   // (N is a multiple of 8)
+                *reinterpret_cast<floats_any *>(p.dY + k * p.dy_pitch + at) = floats_any{0, 0, 0, 0};
+        }
+    }
+}
+
+// Everything in one launch: first the workgroups of dX, then those of dY, which fill up the last round of the first, then the zeros, which take no matrix instructions
+// (ahead of the products 2048 x 16384 x 4096 with a tenth of the rows takes 234 us for 214, floats 552 for 522; in a launch of their own 203 and 696, and
+// 1024 x 4096 x 4096 bf16 with a quarter 79 for 68).
+struct GradWork {
+    GradParams x, y;
+    uint32_t groups_x, groups_y;   // of each; the first a multiple of eight: an XCD gets every eighth workgroup of either
+    ClearParams zeros;
+};
+template <typename T, int WR, int WL, int FR, int FL>
+__global__ __launch_bounds__(64 * WR * WL, 2) void mmm_grad_kernel(const GradWork w)
+{
+    __shared__ __align__(16) char lds[2][256 * (FL * WL + FR * WR) * 8];
+    if (blockIdx.x < w.groups_x)
+        gradient<T, true, WR, WL, FR, FL>(w.x, blockIdx.x, lds);
+    else if (blockIdx.x < w.groups_x + w.groups_y)
+        gradient<T, false, WR, WL, FR, FL>(w.y, blockIdx.x - w.groups_x, lds);
+    else
+        clear<(int)sizeof(T)>(w.zeros, blockIdx.x - w.groups_x - w.groups_y);
+}
+
 // The sums of a split contraction, in the order of its parts.
-template <typename T, bool TO_X> __global__ __launch_bounds__(256) void mmm_grad_join_kernel(const GradParams p)
+template <typename T, bool TO_X> __device__ __forceinline__ void join(const GradParams &p)
 {
     const uint32_t live = p.kinfo != nullptr ? *p.kinfo : (uint32_t)p.K;
     const uint32_t size_r = TO_X ? live : (uint32_t)p.N, size_l = TO_X ? (uint32_t)p.M : live;
@@ -357,31 +414,12 @@ template <typename T, bool TO_X> __global__ __launch_bounds__(256) void mmm_grad
         store_results<T, TO_X>(p, l, r, live, sum);
     }
 }
-
-// Row-compacted mode: zeros where no tile writes, in one launch.  dX: everything (its results lie here and there in its rows); dY: the rows
-// that are off.
-struct ClearParams {
-    char *dX, *dY;   // null: not asked for
-    int64_t dx_pitch, dx_bytes, M, dy_pitch, dy_bytes, K;
-    const uint64_t *rows;
-};
-__global__ __launch_bounds__(256) void mmm_grad_clear_kernel(const ClearParams p)
+template <typename T> __global__ __launch_bounds__(256) void mmm_grad_join_kernel(const GradParams x, const GradParams y)
 {
-    typedef AnyPiece<2>::type piece_any;
-    typedef uint16_t half_any __attribute__((may_alias));
-    const bool of_y = blockIdx.z != 0 || p.dX == nullptr;
-    char *const out = of_y ? p.dY : p.dX;
-    const int64_t pitch = of_y ? p.dy_pitch : p.dx_pitch, bytes = of_y ? p.dy_bytes : p.dx_bytes, rows = of_y ? p.K : p.M;
-    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-        if (of_y && (p.rows[row >> 6] >> (row & 63) & 1ull)) continue;
-        for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16; at < bytes; at += (int64_t)gridDim.x * 256 * 16) {
-            char *const to = out + row * pitch + at;
-            if (at + 16 <= bytes)
-                *reinterpret_cast<piece_any *>(to) = piece_any{0, 0, 0, 0};
-            else
-                for (int64_t q = 0; at + q < bytes; q += 2) *reinterpret_cast<half_any *>(to + q) = 0;
-        }
-    }
+    if (blockIdx.z == 0 && x.splits > 1)
+        join<T, true>(x);
+    else
+        join<T, false>(y);
 }
 
 // Tile and split of the contraction.  The larger a tile, the fewer operands it takes from LDS per product (256 x 256: as many cycles of LDS as of
@@ -397,52 +435,110 @@ constexpr TileCost kTiles16[] = {{64, 4, 7.5, 0.32, 0.245}, {128, 2, 9.5, 0.69, 
 constexpr TileCost kTilesFloat[] = {{64, 4, 7.6, 0.72, 0.59}, {128, 2, 9.9, 2.18, 2.18}, {256, 1, 14.3, 7.57, 7.57}};
 constexpr double kJoin = 1.5, kJoinPerMB = 0.3;
 
-struct GradPlan { int tile; int32_t splits, steps_per_split; };
-// rows_bytes: from a row of dC to the next; a tile's rows lie within 2^31 bytes
-GradPlan plan_grad(int64_t size_r, int64_t size_l, int64_t steps, bool floats, size_t room, size_t bytes_per_split, int64_t row_bytes)
+constexpr int32_t kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+
+// A gradient: its extent along R and L, the steps of its contraction, and the bytes of partial sums for each part of it.
+struct GradJob {
+    int64_t size_r, size_l, steps;
+    size_t bytes;
+    int64_t tiles(int64_t tile) const { return ((size_r + tile - 1) / tile) * ((size_l + tile - 1) / tile); }
+    int64_t steps_of(int32_t want) const { return (steps + want - 1) / want; }
+    int32_t parts_of(int32_t want) const { return (int32_t)((steps + steps_of(want) - 1) / steps_of(want)); }   // (no part is empty)
+    double megabytes() const { return (double)size_r * (double)size_l * 4e-6; }
+};
+struct GradPlan { int tile; int32_t splits, steps_per_split; double us; };
+
+// By itself.  row_bytes: from a row of dC to the next; a tile's rows lie within 2^31 bytes
+GradPlan plan_one(const GradJob &j, bool floats, size_t room, int64_t row_bytes)
 {
-    GradPlan best{};
-    double least = -1.0;
+    GradPlan best{0, 0, 0, -1.0};
     for (const TileCost &c : floats ? kTilesFloat : kTiles16) {
         if (c.tile > 128 && c.tile * row_bytes >= 0x80000000LL) continue;
-        const int64_t tiles = ((size_r + c.tile - 1) / c.tile) * ((size_l + c.tile - 1) / c.tile);
-        for (int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-            if (want > 1 && ((size_t)want * bytes_per_split > room || steps < want)) break;
-            const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;   // no part is empty
-            const int64_t round = 256 * c.at_once, left = tiles * splits % round;
-            const double rounds = (double)(tiles * splits / round) * std::max(c.alone, c.busy * c.at_once) +
+        for (int32_t want : kParts) {
+            if (want > 1 && ((size_t)want * j.bytes > room || j.steps < want)) break;
+            const int64_t per = j.steps_of(want), splits = j.parts_of(want), groups = j.tiles(c.tile) * splits, round = 256 * c.at_once, left = groups % round;
+            const double rounds = (double)(groups / round) * std::max(c.alone, c.busy * c.at_once) +
                                   (left != 0 ? std::max(c.alone, c.busy * (double)((left + 255) / 256)) : 0.0);
-            const double us = c.fixed + (double)per * rounds + (splits > 1 ? kJoin + (double)splits * (double)size_r * (double)size_l * 4e-6 * kJoinPerMB : 0.0);
-            if (least < 0.0 || us < least) {
-                least = us;
-                best = {c.tile, (int32_t)splits, (int32_t)per};
-            }
+            const double us = c.fixed + (double)per * rounds + (splits > 1 ? kJoin + (double)splits * j.megabytes() * kJoinPerMB : 0.0);
+            if (best.us < 0.0 || us < best.us) best = {c.tile, (int32_t)splits, (int32_t)per, us};
         }
     }
     return best;
 }
 
-template <typename T, bool TO_X> hipError_t launch(const mmm_maps *m, GradParams p, hipStream_t s)
+// Both in one launch, with the smallest tile: the workgroups of one fill what those of the other leave idle, and a launch (and a join) is saved.  Estimate: the steps of
+// all workgroups spread over the machine, and a share of the longest chain; fitted to 19 shapes of each element type and 36 pairs of parts (16 x 200 x 16384 to 512 x 8192 x
+// 4096, off by 11 and 6 %).  Taken where it promises less than two launches: 17 (16-bit) and 10 % (floats) less time than these over the shapes, up to 39 % less; not where
+// there is work for larger tiles (512 x 8192 x 4096 bf16: 117 us in two, 131 in one) or little more than writing dY (16 x 4096 x 4096: 33 and 37).
+struct BothCost { double fixed, step, longest, join, join_per_mb, write_per_mb; };
+constexpr BothCost kBoth16{5.05, 0.139, 0.228, 2.23, 0.33, 0.39}, kBothFloat{5.9, 0.48, 0.42, 2.1, 0.27, 0.29};
+
+bool plan_both(const GradJob &x, const GradJob &y, bool floats, size_t room, GradPlan &plan_x, GradPlan &plan_y)
 {
-    const int64_t size_r = TO_X ? m->K : m->N, size_l = TO_X ? m->M : m->K;
-    // row-compacted mode: as many k as the most recent count has found (a guess: the kernels go by the number the device has)
-    const int64_t live = m->b_compact && m->stats_b_valid ? std::max<int64_t>(1, std::min<int64_t>(m->K, (int64_t)m->stats_rows_b)) : m->K;
-    const GradPlan plan = plan_grad(TO_X ? live : size_r, TO_X ? size_l : live, p.steps, sizeof(T) == 4, m->partial_bytes,
-                                    (size_t)((size_r + 3) & ~3LL) * (size_t)size_l * sizeof(float), p.lddc * (int64_t)sizeof(T));
-    const int64_t tiles = ((size_r + plan.tile - 1) / plan.tile) * ((size_l + plan.tile - 1) / plan.tile) * plan.splits;
-    if (tiles > (1LL << 32) / 512 - 1) return hipErrorInvalidValue;   // threads of a launch
-    p.splits = plan.splits;
-    p.steps_per_split = plan.steps_per_split;
-    p.partials = m->partials;
-    void (*fn)(const GradParams) = plan.tile == 256   ? mmm_grad_kernel<T, TO_X, 2, 4, 8, 4>
-                                   : plan.tile == 128 ? mmm_grad_kernel<T, TO_X, 2, 2, 4, 4>
-                                                      : mmm_grad_kernel<T, TO_X, 2, 2, 2, 2>;
-    hipLaunchKernelGGL(fn, dim3((uint32_t)tiles), dim3(plan.tile == 256 ? 512 : 256), 0, s, p);
-    if (plan.splits > 1) {
-        const dim3 grid((uint32_t)((size_r + 1023) / 1024), (uint32_t)std::min<int64_t>(size_l, 65535));
-        hipLaunchKernelGGL((mmm_grad_join_kernel<T, TO_X>), grid, dim3(256), 0, s, p);
+    constexpr int TILE = 64;
+    const BothCost &c = floats ? kBothFloat : kBoth16;
+    double least = plan_x.us + plan_y.us;
+    bool together = false;
+    for (int32_t want_x : kParts)
+        for (int32_t want_y : kParts) {
+            if (x.steps < want_x || y.steps < want_y) break;
+            const int64_t per_x = x.steps_of(want_x), per_y = y.steps_of(want_y);
+            const int32_t splits_x = x.parts_of(want_x), splits_y = y.parts_of(want_y);
+            const double of_x = splits_x > 1 ? splits_x : 0, of_y = splits_y > 1 ? splits_y : 0;   // parts that are joined
+            if ((size_t)of_x * x.bytes + (size_t)of_y * y.bytes > room) break;
+            const double work = (double)(x.tiles(TILE) * splits_x * per_x + y.tiles(TILE) * splits_y * per_y) / 256.0;
+            const double us = c.fixed + c.step * work + c.longest * (double)std::max(per_x, per_y) + c.write_per_mb * (x.megabytes() + y.megabytes()) +
+                              (of_x + of_y > 0 ? c.join + c.join_per_mb * (of_x * x.megabytes() + of_y * y.megabytes()) : 0.0);
+            if (us >= least) continue;
+            least = us;
+            together = true;
+            plan_x = {TILE, splits_x, (int32_t)per_x, us};
+            plan_y = {TILE, splits_y, (int32_t)per_y, us};
+        }
+    return together;
+}
+
+// Those gradients that are planned, of one tile.
+template <typename T> hipError_t launch(const mmm_maps *m, GradWork w, const GradPlan *x, const GradPlan *y, size_t bytes_x, hipStream_t s)
+{
+    const int tile = x != nullptr ? x->tile : y->tile;
+    auto groups_of = [&](GradParams &p, const GradPlan &plan, int64_t r, int64_t l) -> int64_t {
+        p.splits = plan.splits;
+        p.steps_per_split = plan.steps_per_split;
+        p.partials = m->partials;
+        return ((r + tile - 1) / tile) * ((l + tile - 1) / tile) * plan.splits;
+    };
+    w.x.splits = w.y.splits = 1;
+    const int64_t groups_x = x != nullptr ? (groups_of(w.x, *x, m->K, m->M) + 7) & ~7LL : 0, groups_y = y != nullptr ? groups_of(w.y, *y, m->N, m->K) : 0;
+    if (w.x.splits > 1) w.y.partials += (size_t)w.x.splits * bytes_x / sizeof(float);
+    const int64_t groups = groups_x + groups_y + w.zeros.groups;
+    if (groups > (1LL << 32) / 512 - 1) return hipErrorInvalidValue;   // threads of a launch
+    w.groups_x = (uint32_t)groups_x;
+    w.groups_y = (uint32_t)groups_y;
+    void (*fn)(const GradWork) = tile == 256 ? mmm_grad_kernel<T, 2, 4, 8, 4> : tile == 128 ? mmm_grad_kernel<T, 2, 2, 4, 4> : mmm_grad_kernel<T, 2, 2, 2, 2>;
+    hipLaunchKernelGGL(fn, dim3((uint32_t)groups), dim3(tile == 256 ? 512 : 256), 0, s, w);
+    if (w.x.splits > 1 || w.y.splits > 1) {
+        const int64_t r = std::max(w.x.splits > 1 ? m->K : 0, w.y.splits > 1 ? m->N : 0), l = std::max(w.x.splits > 1 ? m->M : 0, w.y.splits > 1 ? m->K : 0);
+        const dim3 grid((uint32_t)((r + 1023) / 1024), (uint32_t)std::min<int64_t>(l, 65535), w.x.splits > 1 && w.y.splits > 1 ? 2 : 1);
+        hipLaunchKernelGGL(mmm_grad_join_kernel<T>, grid, dim3(256), 0, s, w.x, w.y);
     }
     return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_wanted(const mmm_maps *m, GradWork w, bool x, bool y, hipStream_t s)
+{
+    // row-compacted mode: as many k as the most recent count has found (a guess: the kernels go by the number the device has)
+    const int64_t live = m->b_compact && m->stats_b_valid ? std::max<int64_t>(1, std::min<int64_t>(m->K, (int64_t)m->stats_rows_b)) : m->K;
+    const auto quads = [](int64_t r) { return (size_t)((r + 3) & ~3LL); };
+    const GradJob job_x{live, m->M, w.x.steps, quads(m->K) * (size_t)m->M * sizeof(float)}, job_y{m->N, live, w.y.steps, quads(m->N) * (size_t)m->K * sizeof(float)};
+    const bool floats = sizeof(T) == 4;
+    GradPlan plan_x = plan_one(job_x, floats, m->partial_bytes, w.x.lddc * (int64_t)sizeof(T)), plan_y = plan_one(job_y, floats, m->partial_bytes, w.x.lddc * (int64_t)sizeof(T));
+    // (planned for both also where one is asked for: its sums are then the same)
+    const bool together = plan_both(job_x, job_y, floats, m->partial_bytes, plan_x, plan_y);
+    if (together || !x || !y) return launch<T>(m, w, x ? &plan_x : nullptr, y ? &plan_y : nullptr, job_x.bytes, s);
+    if (const hipError_t e = launch<T>(m, w, &plan_x, nullptr, job_x.bytes, s); e != hipSuccess) return e;
+    w.zeros = {};   // (are written)
+    return launch<T>(m, w, nullptr, &plan_y, job_x.bytes, s);
 }
 
 }   // namespace
@@ -470,29 +566,20 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
     p.accumulate = accumulate;
     p.parts = m->a_form == MMM_FORM_PARTS;
     const int64_t esz = dtype == MMM_F32 ? 4 : 2;
-    (void)hipGetLastError();
+    GradWork w{p, p, 0, 0, {}};
+    w.x.out = dX;
+    w.x.ldo = lddx;
+    w.x.steps = (int32_t)((m->N * esz + ROWB - 1) / ROWB);
+    w.y.out = dY;
+    w.y.ldo = lddy;
+    w.y.steps = (int32_t)(m->MBA * (dtype == MMM_F32 ? 2 : 1));
     const bool clear_y = dY != nullptr && !accumulate;
     if (m->b_compact && (dX != nullptr || clear_y)) {
-        const ClearParams c{static_cast<char *>(dX), clear_y ? reinterpret_cast<char *>(dY) : nullptr, lddx * esz, m->K * esz, m->M, lddy * 4, m->N * 4, m->K, m->rows_copy};
-        const int64_t bytes = std::max(dX != nullptr ? c.dx_bytes : 0, clear_y ? c.dy_bytes : 0), rows = std::max(dX != nullptr ? c.M : 0, clear_y ? c.K : 0);
-        // some 2048 workgroups that go from row to row (one for each row: 11.4 us for 777 x 3001 and 3001 x 1992 floats, so 7.8)
-        const uint32_t across = (uint32_t)std::min<int64_t>((bytes + 4095) / 4096, 16), both = dX != nullptr && clear_y ? 2 : 1;
-        const dim3 grid(across, (uint32_t)std::min<int64_t>(rows, 2048 / (across * both)), both);
-        hipLaunchKernelGGL(mmm_grad_clear_kernel, grid, dim3(256), 0, s, c);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        const int64_t rows = (dX != nullptr ? m->M : 0) + (clear_y ? m->K : 0);
+        w.zeros = {static_cast<char *>(dX), clear_y ? reinterpret_cast<char *>(dY) : nullptr, lddx * esz, m->M, lddy * 4, m->N * 4, m->K, m->rows_copy,
+                   (uint32_t)std::min<int64_t>(rows, 1024)};
     }
-    if (dX != nullptr) {
-        p.out = dX;
-        p.ldo = lddx;
-        p.steps = (int32_t)((m->N * esz + ROWB - 1) / ROWB);
-        const hipError_t e = dtype == MMM_F32 ? launch<float, true>(m, p, s) : dtype == MMM_BF16 ? launch<__bf16, true>(m, p, s) : launch<_Float16, true>(m, p, s);
-        if (e != hipSuccess) return e;
-    }
-    if (dY != nullptr) {
-        p.out = dY;
-        p.ldo = lddy;
-        p.steps = (int32_t)(m->MBA * (dtype == MMM_F32 ? 2 : 1));
-        return dtype == MMM_F32 ? launch<float, false>(m, p, s) : dtype == MMM_BF16 ? launch<__bf16, false>(m, p, s) : launch<_Float16, false>(m, p, s);
-    }
-    return hipSuccess;
+    (void)hipGetLastError();
+    const bool x = dX != nullptr, y = dY != nullptr;
+    return dtype == MMM_F32 ? launch_wanted<float>(m, w, x, y, s) : dtype == MMM_BF16 ? launch_wanted<__bf16>(m, w, x, y, s) : launch_wanted<_Float16>(m, w, x, y, s);
 }
