@@ -378,8 +378,10 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
                     }
                 };
                 uint32_t t = 0;
-                if (FUSED)
+                if (FUSED) {
+                    for (; t + 6 * C16 < rmax; t += 8 * C16) batch(t, std::integral_constant<int, 8>{});
                     for (; t + 2 * C16 < rmax; t += 4 * C16) batch(t, std::integral_constant<int, 4>{});
+                }
                 for (; t + C16 < rmax; t += 2 * C16) batch(t, std::integral_constant<int, 2>{});
                 if (t < rmax) batch(t, std::integral_constant<int, 1>{});
             }
@@ -431,7 +433,7 @@ struct PairsShape { int cw, ks, words; };
 // Workgroup shapes: CW waves side by side (64 columns each), KS that share K, and the map words a wave intersects at a time.
 //   8 x 1  512 columns: many rows, or a K so short that there is nothing to share out
 //   2 x 4  few rows: 128 columns, K in four shares
-//   8 x 2, 4 x 4, 2 x 8  few rows, mask evaluated here: the predicate work is shared by 512, 256, 128 columns
+//   8 x 2, 4 x 4, 2 x 8, 1 x 8  few rows, mask evaluated here: the predicate work is shared by 512, 256, 128, 64 columns
 // Words: the fewest that still give every share a part of K (64 k each), so that no wave stands idle: a K of 4096 in ranges
 // of 64 words was one range, for one wave in four.
 template <typename T, int BW, bool FUSED, bool EPI> pairs_kernel_fn<EPI> pick_shape(const PairsShape &sh)
@@ -443,6 +445,7 @@ template <typename T, int BW, bool FUSED, bool EPI> pairs_kernel_fn<EPI> pick_sh
     if constexpr (!FUSED) {
         return w == 16 ? mmm_pairs_kernel<T, BW, 2, 4, W16, FUSED, EPI> : w == 32 ? mmm_pairs_kernel<T, BW, 2, 4, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 2, 4, 64, FUSED, EPI>;
     } else {
+        if (sh.cw == 1) return w == 16 ? mmm_pairs_kernel<T, BW, 1, 8, W16, FUSED, EPI> : mmm_pairs_kernel<T, BW, 1, 8, 32, FUSED, EPI>;
         if (sh.ks == 8) return w == 16 ? mmm_pairs_kernel<T, BW, 2, 8, W16, FUSED, EPI> : mmm_pairs_kernel<T, BW, 2, 8, 32, FUSED, EPI>;
         if (sh.ks == 4) return w <= 32 ? mmm_pairs_kernel<T, BW, 4, 4, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 4, 4, 64, FUSED, EPI>;
         return w <= 32 ? mmm_pairs_kernel<T, BW, 8, 2, 32, FUSED, EPI> : mmm_pairs_kernel<T, BW, 8, 2, 64, FUSED, EPI>;
@@ -492,12 +495,15 @@ static hipError_t launch_pairs(const mmm_maps *m, int32_t dtype, const void *X, 
     // Workgroups of 8 waves x 64 columns; when that gives the machine too little to do (few rows:
     // the decode shape), fewer columns per workgroup and K shared out over several waves, unless there is next to nothing of it.
     // With the mask evaluated here every column span repeats the predicate, so the spans are as wide as leaves every compute unit a
-    // workgroup (4 x 16384 x 4096 bf16: 128, 256 columns: 5.7, 6.6 us; 16 x 8192 x 4096, where 128 make two rounds: 8.7, 5.6).
+    // workgroup (4 x 16384 x 4096 bf16: 64, 128, 256 columns: 6.6, 7.1, 8.0 us back to back; 8 x 8192 x 2048 floats: 64, 128: 10.5, 13.8; 1 x 11740 x 328 floats, all
+    // elements on: 23, 41; 16 x 8192 x 4096 bf16, where 128 make two rounds: 8.7, 256: 5.6).  Columns do not change the order of a sum.
     const int64_t wide = (m->N + 511) / 512 * m->M;
     PairsShape sh{8, 1, 64};
     if (wide < 1024 && (fused || m->WA > 32)) {
         if (!fused)
             sh = {2, 4, 64};
+        else if ((m->N + 63) / 64 * m->M <= 256)
+            sh = {1, 8, 32};
         else if ((m->N + 127) / 128 * m->M <= 256)
             sh = {2, 8, 32};
         else if (m->M <= 16)
