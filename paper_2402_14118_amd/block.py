@@ -11,7 +11,7 @@ import torch
 
 from . import binding as B
 from .engine import MaskedMatmul
-from .tensors import TORCH_TYPES, check_device, own_device, rows
+from .tensors import TORCH_TYPES, check_device, own_device, places
 
 
 class BlockNorm:
@@ -28,33 +28,28 @@ class BlockNorm:
                  alpha: float = 1.0, eps: float = 1e-5, dtype_h: Optional[int] = None, dtype_y: Optional[int] = None, training: bool = False,
                  device="cuda:0"):
         self.desc = B.BlockNormDesc(M, N, dtype, dtype if dtype_h is None else dtype_h, dtype if dtype_y is None else dtype_y, post, pre, gate, eps, alpha)
-        self.dtype, self.dtype_h, self.dtype_y, self.shape, self.columns = dtype, self.desc.dt_h, self.desc.dt_y, (M, N), (N,)
+        # shapes and types of the operands
+        self.shape, self.columns = (M, N), (N,)
+        self.gate_shape = {B.MMM_GATE_ROW: (M,), B.MMM_GATE_COL: (N,), B.MMM_GATE_FULL: (M, N)}.get(gate)
+        self.type, self.type_h, self.type_y = (TORCH_TYPES.get(t) for t in (dtype, self.desc.dt_h, self.desc.dt_y))
+        self.type_grad_gate = self.type if gate == B.MMM_GATE_FULL else torch.float32
         self.device = own_device(device)
         nbytes = B.mmm_block_norm_backward_workspace_bytes(M, N)   # (checks M and N)
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if training else None
         self.room = (self.workspace.data_ptr(), nbytes) if training else (None, 0)
         self.fields = self.desc.fields()
 
-    def _gate(self, name, t, sums=False):
-        d = self.desc
-        shape = {B.MMM_GATE_ROW: (d.M,), B.MMM_GATE_COL: (d.N,), B.MMM_GATE_FULL: (d.M, d.N)}.get(d.gate)
-        if shape is None and t is not None:
-            raise ValueError(f"{name} is given, but there is no gate")
-        return rows(name, t, shape, B.MMM_F32 if sums and d.gate != B.MMM_GATE_FULL else d.dt, self.device)
-
     def forward(self, H: torch.Tensor, normed: Optional[torch.Tensor] = None, H_out: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
                 gate: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
                 pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
         """H_out may be H."""
-        dt, dev, shape = self.dtype, self.device, self.shape
-        check_device(dev)
-        h, ldh = rows("H", H, shape, self.dtype_h, dev, False)
-        y, ldy = rows("Y", Y, shape, self.dtype_y, dev)
-        g, ldg = self._gate("gate", gate) if gate is not None else (None, 0)
-        ho, ldho = rows("H_out", H_out, shape, self.dtype_h, dev)
-        n, ldn = rows("normed", normed, shape, dt, dev)
-        pw, pb, w, b = (None if t is None else rows(name, t, self.columns, dt, dev)[0] for name, t in
-                        (("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight), ("pre_bias", pre_bias)))
+        t, th, shape, columns = self.type, self.type_h, self.shape, self.columns
+        check_device(self.device)
+        if gate is not None and self.gate_shape is None:
+            raise ValueError("gate is given, but there is no gate")
+        h, ldh, y, ldy, g, ldg, pw, _, pb, _, w, _, b, _, ho, ldho, n, ldn = places(
+            self.device, 1, ("H", "Y", "gate", "post_weight", "post_bias", "pre_weight", "pre_bias", "H_out", "normed"), H, shape, th, Y, shape, self.type_y,
+            gate, self.gate_shape, t, post_weight, columns, t, post_bias, columns, t, pre_weight, columns, t, pre_bias, columns, t, H_out, shape, th, normed, shape, t)
         B._check(B.native.block_norm(self.fields, h, ldh, y, ldy, g, ldg, pw, pb, w, b, ho, ldho, n, ldn, B._stream(stream)), "mmm_block_norm")
 
     def backward(self, H_out: Optional[torch.Tensor] = None, grad_normed: Optional[torch.Tensor] = None, grad_H_out: Optional[torch.Tensor] = None,
@@ -65,22 +60,17 @@ class BlockNorm:
                  grad_pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
         """H_out: as the forward call left it (H where there was no block).  grad_H may be grad_H_out.  Gradients that are not given are
         not worked out; those of weights, biases and of a gate per row or column are float."""
-        dt, dev, shape, columns, f = self.dtype, self.device, self.shape, self.columns, B.MMM_F32
-        check_device(dev)
-        ho, ldho = rows("H_out", H_out, shape, self.dtype_h, dev)
-        y, ldy = rows("Y", Y, shape, self.dtype_y, dev)
-        ga, ldga = self._gate("gate", gate) if gate is not None else (None, 0)
-        dn, lddn = rows("grad_normed", grad_normed, shape, dt, dev)
-        dho, lddho = rows("grad_H_out", grad_H_out, shape, self.dtype_h, dev)
-        dh, lddh = rows("grad_H", grad_H, shape, self.dtype_h, dev)
-        dy, lddy = rows("grad_Y", grad_Y, shape, self.dtype_y, dev)
-        dg, lddg = self._gate("grad_gate", grad_gate, sums=True) if grad_gate is not None else (None, 0)
-        pw, pb, w = (None if t is None else rows(name, t, columns, dt, dev)[0] for name, t in
-                     (("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight)))
-        sums = (None if t is None else rows(name, t, columns, f, dev)[0] for name, t in
-                (("grad_post_weight", grad_post_weight), ("grad_post_bias", grad_post_bias), ("grad_pre_weight", grad_pre_weight),
-                 ("grad_pre_bias", grad_pre_bias)))
-        B._check(B.native.block_norm_backward(self.fields, ho, ldho, y, ldy, ga, ldga, pw, pb, w, dn, lddn, dho, lddho, dh, lddh, dy, lddy, dg, lddg, *sums,
+        t, th, ty, shape, columns, f = self.type, self.type_h, self.type_y, self.shape, self.columns, torch.float32
+        check_device(self.device)
+        if self.gate_shape is None and (gate is not None or grad_gate is not None):
+            raise ValueError("gate is given, but there is no gate")
+        (ho, ldho, y, ldy, ga, ldga, pw, _, pb, _, w, _, dn, lddn, dho, lddho, dh, lddh, dy, lddy, dg, lddg, dpw, _, dpb, _, dw, _, db, _) = places(
+            self.device, 0, ("H_out", "Y", "gate", "post_weight", "post_bias", "pre_weight", "grad_normed", "grad_H_out", "grad_H", "grad_Y", "grad_gate",
+                             "grad_post_weight", "grad_post_bias", "grad_pre_weight", "grad_pre_bias"),
+            H_out, shape, th, Y, shape, ty, gate, self.gate_shape, t, post_weight, columns, t, post_bias, columns, t, pre_weight, columns, t,
+            grad_normed, shape, t, grad_H_out, shape, th, grad_H, shape, th, grad_Y, shape, ty, grad_gate, self.gate_shape, self.type_grad_gate,
+            grad_post_weight, columns, f, grad_post_bias, columns, f, grad_pre_weight, columns, f, grad_pre_bias, columns, f)
+        B._check(B.native.block_norm_backward(self.fields, ho, ldho, y, ldy, ga, ldga, pw, pb, w, dn, lddn, dho, lddho, dh, lddh, dy, lddy, dg, lddg, dpw, dpb, dw, db,
                                               *self.room, B._stream(stream)), "mmm_block_norm_backward")
 
 
@@ -135,8 +125,8 @@ class MaskedMlp:
                     keep_rows2: Optional[torch.Tensor] = None, stream=None) -> None:
         """Build the maps of both weights; again after a weight or a selection has changed."""
         check_device(self.device)
-        rows("W1", W1, (self.width, self.hidden), self.dtype, self.device, False)
-        rows("W2", W2, (self.hidden, self.width), self.dtype, self.device, False)
+        t = TORCH_TYPES[self.dtype]
+        places(self.device, 2, ("W1", "W2", "b1", "b2"), W1, (self.width, self.hidden), t, W2, (self.hidden, self.width), t, b1, (self.hidden,), t, b2, (self.width,), t)
         self.W1, self.W2, self.b1, self.b2 = W1, W2, b1, b2
         self.up.build_maps(None, W1, keep_blocks=keep_blocks1, stream=stream)
         self.down.build_maps(None, W2, keep_rows=keep_rows2, keep_blocks=keep_blocks2, stream=stream)
@@ -152,7 +142,7 @@ class MaskedMlp:
         """H_out may be H (backward() does not need H); normed receives n'."""
         if self.W1 is None:
             raise ValueError("set_weights() comes first")
-        rows("N", N, (self.M, self.width), self.dtype, self.device, False)
+        places(self.device, 1, ("N",), N, (self.M, self.width), TORCH_TYPES[self.dtype])
         kept = self.preact if self.training and self.preact is not self.a else None
         self.up.build_maps(N, None, stream=stream)
         self.up.matmul_epilogue(N, self.W1, self.a, bias=self.b1, activation=self.activation, preact=kept, stream=stream)
@@ -171,14 +161,13 @@ class MaskedMlp:
         if not self.training:
             raise ValueError("made without training=True")
         M, ws, od = self.M, self.workspace, self.dtype
+        places(self.device, 0, ("grad_b1", "grad_b2"), grad_b1, (self.hidden,), torch.float32, grad_b2, (self.width,), torch.float32)
         self.norm.backward(H_out=H_out, grad_normed=grad_normed, grad_H_out=grad_H_out, grad_H=grad_H, Y=self.y, grad_Y=self.grad_y, stream=stream, **norm)
         if grad_b2 is not None:
-            rows("grad_b2", grad_b2, (self.width,), B.MMM_F32, self.device)
             B.mmm_epilogue_backward(M, self.width, od, od, B.MMM_ACT_NONE, self.grad_y, self.width, None, 0, None, 0, grad_b2, ws, ws.numel(), stream)
         # (a unit that ReLU has turned off has no slope; elsewhere a zero is a value like others)
         self.down.matmul_backward(self.a, self.W2, self.grad_y, dX=self.grad_a, dY=grad_W2, accumulate=accumulate,
                                   all_x=self.activation != B.MMM_ACT_RELU, stream=stream)
-        rows("grad_b1", grad_b1, (self.hidden,), B.MMM_F32, self.device)
         B.mmm_epilogue_backward(M, self.hidden, od, od, self.activation, self.grad_a, self.hidden, self.preact, self.hidden, self.grad_a, self.hidden,
                                 grad_b1, ws, ws.numel(), stream)
         self.up.matmul_backward(N, self.W1, self.grad_a, dX=grad_N, dY=grad_W1, accumulate=accumulate, all_x=True, stream=stream)

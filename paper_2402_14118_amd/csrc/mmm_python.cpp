@@ -291,19 +291,17 @@ PyObject *block_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
-// place(tensor, shape, dtype, device): (address, leading dimension) of a matrix (leading dimension 0: of a vector) that has this shape, type and device
-// and whose elements are neighbours; None where anything differs (the caller then says what).
-PyObject *place(PyObject *, PyObject *const *v, Py_ssize_t n)
+// The address (a new reference) and the leading dimension of a matrix (0: of a vector) that has this shape, type and device and whose elements are
+// neighbours; null where anything differs.
+PyObject *located(PyObject *t, PyObject *want, PyObject *type, PyObject *where, long long &ld)
 {
-    if (!arity("place", n, 4)) return nullptr;
     static PyObject *const shape_name = PyUnicode_InternFromString("shape"), *const dtype_name = PyUnicode_InternFromString("dtype"),
                            *const device_name = PyUnicode_InternFromString("device"), *const stride_name = PyUnicode_InternFromString("stride"),
                            *const address_name = PyUnicode_InternFromString("data_ptr");
-    PyObject *const t = v[0], *const want = v[1];
-    long long ld = -1;
+    ld = -1;
     PyObject *const shape = PyObject_GetAttr(t, shape_name), *const dtype = PyObject_GetAttr(t, dtype_name), *const device = PyObject_GetAttr(t, device_name);
     PyObject *stride = nullptr, *address = nullptr;
-    if (shape != nullptr && device != nullptr && PyTuple_Check(shape) && PyTuple_Check(want) && dtype == v[2]) {
+    if (shape != nullptr && device != nullptr && PyTuple_Check(shape) && PyTuple_Check(want) && dtype == type) {
         const Py_ssize_t dims = PyTuple_GET_SIZE(want);
         bool same = (dims == 1 || dims == 2) && PyTuple_GET_SIZE(shape) == dims;
         long long size[2] = {1, 1};
@@ -311,7 +309,7 @@ PyObject *place(PyObject *, PyObject *const *v, Py_ssize_t n)
             size[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(want, i));
             same = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i)) == size[i];
         }
-        if (same && PyObject_RichCompareBool(device, v[3], Py_EQ) == 1) stride = PyObject_CallMethodNoArgs(t, stride_name);
+        if (same && PyObject_RichCompareBool(device, where, Py_EQ) == 1) stride = PyObject_CallMethodNoArgs(t, stride_name);
         if (stride != nullptr && PyTuple_Check(stride) && PyTuple_GET_SIZE(stride) == dims) {
             const long long last = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, dims - 1)), first = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0));
             if (last == 1 || size[dims - 1] <= 1) ld = dims == 1 ? 0 : size[0] > 1 || first > size[1] ? first : size[1];
@@ -322,18 +320,43 @@ PyObject *place(PyObject *, PyObject *const *v, Py_ssize_t n)
     Py_XDECREF(dtype);
     Py_XDECREF(device);
     Py_XDECREF(stride);
-    PyErr_Clear();
-    if (address == nullptr) Py_RETURN_NONE;
-    PyObject *const both = PyTuple_New(2), *const leading = PyLong_FromLongLong(ld);
-    if (both == nullptr || leading == nullptr) {
-        Py_XDECREF(both);
-        Py_XDECREF(leading);
-        Py_DECREF(address);
+    if (address == nullptr) PyErr_Clear();
+    return address;
+}
+
+// places(device, needed, tensor, shape, dtype, tensor, shape, dtype, ...): (address, leading dimension, address, leading dimension, ...) of all, None and 0 of a
+// tensor that is None; the first `needed` have to be there.  Where something is wrong, the number of that tensor.
+PyObject *places(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    if (n < 2 || (n - 2) % 3 != 0) {
+        PyErr_SetString(PyExc_TypeError, "places takes a device, a number and three arguments for each tensor");
         return nullptr;
     }
-    PyTuple_SET_ITEM(both, 0, address);
-    PyTuple_SET_ITEM(both, 1, leading);
-    return both;
+    const Py_ssize_t tensors = (n - 2) / 3;
+    const long long needed = PyLong_AsLongLong(v[1]);
+    if (needed == -1 && PyErr_Occurred()) return nullptr;
+    PyObject *const out = PyTuple_New(2 * tensors);
+    if (out == nullptr) return nullptr;
+    for (Py_ssize_t i = 0; i < tensors; ++i) {
+        PyObject *const *const at = v + 2 + 3 * i;
+        long long ld = 0;
+        PyObject *address = nullptr;
+        if (at[0] == Py_None && i >= needed) {
+            Py_INCREF(Py_None);
+            address = Py_None;
+        } else if (at[0] != Py_None) {
+            address = located(at[0], at[1], at[2], v[0], ld);
+        }
+        PyObject *const leading = address != nullptr ? PyLong_FromLongLong(ld) : nullptr;
+        if (leading == nullptr) {
+            Py_XDECREF(address);
+            Py_DECREF(out);
+            return PyErr_Occurred() ? nullptr : PyLong_FromSsize_t(i);
+        }
+        PyTuple_SET_ITEM(out, 2 * i, address);
+        PyTuple_SET_ITEM(out, 2 * i + 1, leading);
+    }
+    return out;
 }
 
 PyMethodDef methods[] = {
@@ -345,7 +368,7 @@ PyMethodDef methods[] = {
     {"epilogue_backward", (PyCFunction)(void (*)(void))epilogue_backward, METH_FASTCALL, nullptr},
     {"matmul_backward", (PyCFunction)(void (*)(void))matmul_backward, METH_FASTCALL, nullptr},
     {"block_norm_backward", (PyCFunction)(void (*)(void))block_norm_backward, METH_FASTCALL, nullptr},
-    {"place", (PyCFunction)(void (*)(void))place, METH_FASTCALL, nullptr},
+    {"places", (PyCFunction)(void (*)(void))places, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -10,7 +10,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from .tensors import CODES, check_device, own_device, rows
+from .tensors import CODES, TORCH_TYPES, check_device, own_device, places
 
 
 class MaskedMatmul:
@@ -68,24 +68,21 @@ class MaskedMatmul:
         """C = activation(A x B + bias) + residual; preact receives A x B + bias.  C, residual and preact are of one type: that of the
         inputs, or float.  residual may be C.  With a predicate M is evaluated inside the multiplication, as in matmul_fused."""
         check_device(self.device)
-        dev, dt, shape, out = self.device, self.dtype, (self.M, self.N), CODES.get(C.dtype, -1)
-        x, ldx = rows("X", X, (self.M, self.K), dt, dev, False)
-        y, ldy = rows("Y", Y, (self.K, self.N), dt, dev, False)
-        c, ldc = rows("C", C, shape, out, dev, False)
-        r, ldr = rows("residual", residual, shape, out, dev)
-        z, ldp = rows("preact", preact, shape, out, dev)
-        b = rows("bias", bias, (self.N,), dt, dev)[0]
+        dt, shape, t, out = self.dtype, (self.M, self.N), TORCH_TYPES[self.dtype], C.dtype
+        x, ldx, y, ldy, c, ldc, r, ldr, z, ldp, b, _ = places(
+            self.device, 3, ("X", "Y", "C", "residual", "preact", "bias"), X, (self.M, self.K), t, Y, (self.K, self.N), t, C, shape, out, residual, shape, out,
+            preact, shape, out, bias, (self.N,), t)
         B._check(B.native.matmul_epilogue(self.maps, dt, x, ldx, pred is not None, 0 if pred is None else pred, threshold, B._ptr(keep_a), y, ldy, c, ldc,
-                                          activation, out, b, r, ldr, z, ldp, B._stream(stream)), "mmm_matmul_epilogue")
+                                          activation, CODES.get(out, -1), b, r, ldr, z, ldp, B._stream(stream)), "mmm_matmul_epilogue")
 
     def matmul_backward(self, X: torch.Tensor, Y: torch.Tensor, dC: torch.Tensor, dX: Optional[torch.Tensor] = None,
                         dY: Optional[torch.Tensor] = None, accumulate: bool = False, all_x: bool = False, stream=None) -> None:
         """The gradients of A x B under the maps as built: dX (type of X; zero where A is, unless all_x asks for every element) and dY (float;
         zero where B has no block, or added to).  X must be the tensor the maps were built from."""
         check_device(self.device)
-        dev, dt, mk, kn = self.device, self.dtype, (self.M, self.K), (self.K, self.N)
-        B.mmm_matmul_backward(self.maps, dt, *rows("X", X, mk, dt, dev, False), *rows("Y", Y, kn, dt, dev, False), *rows("dC", dC, (self.M, self.N), dt, dev, False),
-                              *rows("dX", dX, mk, dt, dev), *rows("dY", dY, kn, B.MMM_F32, dev), accumulate, all_x, stream)
+        dt, mk, kn, t = self.dtype, (self.M, self.K), (self.K, self.N), TORCH_TYPES[self.dtype]
+        at = places(self.device, 3, ("X", "Y", "dC", "dX", "dY"), X, mk, t, Y, kn, t, dC, (self.M, self.N), t, dX, mk, t, dY, kn, torch.float32)
+        B._check(B.native.matmul_backward(self.maps, dt, *at, int(accumulate), int(all_x), B._stream(stream)), "mmm_matmul_backward")
 
     def set_path(self, path: int = -1) -> None:
         B.mmm_maps_set_path(self.maps, path)

@@ -1,8 +1,6 @@
 """Tensors as the C ABI takes them: checks of shape, type, device and layout, and the leading dimension."""
 from __future__ import annotations
 
-from typing import Optional
-
 import torch
 
 from . import binding as B
@@ -11,22 +9,22 @@ TORCH_TYPES = {B.MMM_F32: torch.float32, B.MMM_BF16: torch.bfloat16, B.MMM_F16: 
 CODES = {t: code for code, t in TORCH_TYPES.items()}
 
 
-def rows(name: str, t: Optional[torch.Tensor], shape, dtype: int, device, optional: bool = True):
-    """(address, leading dimension) of a matrix, or of a vector (leading dimension 0); (None, 0) of none."""
-    if t is None:
-        if not optional:
-            raise ValueError(f"{name} is needed")
-        return None, 0
-    at = B.native.place(t, shape, TORCH_TYPES.get(dtype), device)
-    if at is not None:
+def places(device, needed: int, names, *tensors):
+    """Tensor, shape and torch type of each in turn; the first `needed` have to be there.  Address and leading dimension (of a vector: 0) of each, one after
+    the other; None and 0 of those that are None."""
+    at = B.native.places(device, needed, *tensors)
+    if type(at) is tuple:
         return at
     # what is wrong with it
+    name, (t, shape, dtype) = names[at], tensors[3 * at:3 * at + 3]
+    if t is None:
+        raise ValueError(f"{name} is needed")
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} is not a tensor")
     if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if CODES.get(t.dtype) != dtype:
-        raise TypeError(f"{name} is {t.dtype}, not {TORCH_TYPES.get(dtype)}")
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {shape if shape is None else tuple(shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
     raise ValueError(f"the elements of {name} are not neighbours in memory")
