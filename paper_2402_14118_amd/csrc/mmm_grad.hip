@@ -18,7 +18,7 @@
 //
 // What bounds it.  Large results: the matrix cores at the clock that the power limit leaves (4096^3 half 1096 TFLOP/s for both, where a library product
 // of 8192^3 bf16 reaches 1140; 2048 x 16384 x 4096 bf16 973; floats 135 of 155).  Small ones: the steps of a workgroup, one after another, and one to four
-// launches.  Rows by context: the zeros of dX and of the rows of dY that are off (2048 x 16384 x 4096 bf16, a tenth of the rows: 214 us, 335 MB of results).
+// launches.  Rows by context: writing the results, most of them zeros (2048 x 16384 x 4096 bf16, a tenth of the rows: 178 us, 335 MB of results).
 // Operands of the smallest tile two steps ahead, in registers: no faster.
 #include <algorithm>
 #include <type_traits>
@@ -49,11 +49,13 @@ struct GradParams {
     const char *a_img;
     const uint64_t *a_bits, *b_bits;
     const uint32_t *kinfo, *kmap;   // row-compacted mode; else null
+    const uint64_t *rows;           // bitmap of the live rows
     int64_t M, K, N, WA, WB;
     int32_t KBA, steps, bw_shift, accumulate;
     int32_t splits, steps_per_split;
     float *partials;     // splits > 1: [split][along L][along R, rows of whole quads]
     bool parts;          // the image is of floats in parts
+    bool whole_rows;     // dX, row-compacted mode: tiles write the zeros between their results as well
 };
 
 // Four neighbouring results along R, from r on, of place l along L; `live`: the number of k there are.
@@ -110,6 +112,87 @@ template <typename T> __device__ __forceinline__ void multiply(const u32x4 &r, c
     }
 }
 
+// dX in row-compacted mode, a tile whose contraction is not split: rows as they are in memory, from the first k of the tile to that of the next one, zeros of
+// the k that are off among them, so that whole lines are written, and once.  Results go through LDS, with the 16-byte pieces of a row turned with it.
+template <typename T, int WR, int WL, int FR, int FL>
+__device__ __forceinline__ void spread_rows(const GradParams &p, const floatx4 (&acc)[FR][FL], uint32_t l0, uint32_t r0, uint32_t live, char (&lds)[2][256 * (FL * WL + FR * WR) * 8])
+{
+    constexpr int ESZ = (int)sizeof(T), TR = 16 * FR * WR, TL = 16 * FL * WL, NW = WR * WL, PER = 16 / ESZ;
+    constexpr int CHUNK = 64 * PER, WORDS = CHUNK / 64;   // k of a wave's store, and words of the map
+    constexpr int AHEAD = 4;                              // rows whose bits are asked for together
+    static_assert(TL * TR * ESZ <= (int)sizeof(lds) && TL % (NW * AHEAD) == 0, "whole turns");
+    typedef typename AnyPiece<ESZ>::type piece_any;
+    typedef T four_t __attribute__((ext_vector_type(4)));
+    typedef four_t four __attribute__((may_alias));
+    typedef T element __attribute__((may_alias));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, s = lane >> 4, wr = wave % WR, wl = wave / WR;
+    char *const room = lds[0];
+    auto place_of = [](uint32_t row, uint32_t col) -> uint32_t { return row * (TR * ESZ) + (((col * ESZ >> 4) ^ (row & 7u)) << 4) + (col * ESZ & 15u); };
+    const uint32_t lo = r0 == 0 ? 0u : p.kmap[r0], hi = r0 + TR < live ? p.kmap[r0 + TR] : (uint32_t)p.K;
+    __syncthreads();   // operands have been read
+#pragma unroll
+    for (int b = 0; b < FL; ++b)
+#pragma unroll
+        for (int a = 0; a < FR; ++a) {
+            four_t v;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = (T)acc[a][b][u];
+            *reinterpret_cast<four *>(room + place_of((uint32_t)((wl * FL + b) * 16 + c), (uint32_t)((wr * FR + a) * 16 + s * 4))) = v;
+        }
+    __syncthreads();
+    uint32_t seen = 0;   // live k of the tile in front of the chunk
+    for (uint32_t k0 = lo & ~63u; k0 < hi; k0 += CHUNK) {
+        // this lane's piece, and which of its k are live; how many of the tile are in front of it
+        const uint32_t k = k0 + (uint32_t)lane * PER, word = min(k, (uint32_t)p.K - 1u) >> 6;
+        uint64_t on = p.rows[word];
+        if (lo > word * 64u) on &= ~0ull << min(lo - word * 64u, 63u);                      // (a word begins at most 63 in front of lo)
+        on = word * 64u >= hi || k >= (uint32_t)p.K ? 0ull : hi - word * 64u < 64u ? on & ((1ull << (hi - word * 64u)) - 1ull) : on;
+        const uint32_t count = (uint32_t)__popcll(on);
+        uint32_t before = seen + (uint32_t)__popcll(on & ((1ull << (k & 63u)) - 1ull));
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            const uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)count, w * (64 / PER));
+            before += w < lane / (64 / PER) ? n : 0u;
+            seen += n;
+        }
+        const uint32_t mine = (uint32_t)(on >> (k & 63u)) & ((1u << PER) - 1u);
+        const bool inside = k >= lo && k + PER <= hi;
+        uint32_t at[PER];
+#pragma unroll
+        for (int q = 0; q < PER; ++q) at[q] = min(before + (uint32_t)__popc(mine & ((1u << q) - 1u)), (uint32_t)TR - 1u);
+        for (uint32_t first = (uint32_t)wave * AHEAD; first < (uint32_t)TL; first += NW * AHEAD) {
+            uint64_t bits[AHEAD];
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                const uint32_t l = min(l0 + first + n, (uint32_t)p.M - 1u);
+                bits[n] = p.a_bits != nullptr ? p.a_bits[(uint64_t)l * (uint64_t)p.WA + word] : ~0ull;
+            }
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                const uint32_t row = first + n, l = l0 + row;
+                if (l >= (uint32_t)p.M) continue;
+                const uint32_t wanted = (uint32_t)(bits[n] >> (k & 63u)) & mine;
+                typedef T piece_t __attribute__((ext_vector_type(PER)));
+                piece_t v;
+#pragma unroll
+                for (int q = 0; q < PER; ++q) {
+                    const T x = *reinterpret_cast<const element *>(room + place_of(row, at[q]));
+                    v[q] = wanted >> q & 1u ? x : (T)0.f;
+                }
+                T *const to = static_cast<T *>(p.out) + (int64_t)l * p.ldo + k;
+                if (inside) {
+                    *reinterpret_cast<piece_any *>(to) = __builtin_bit_cast(u32x4, v);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < PER; ++q)
+                        if (k + q >= lo && k + q < hi) to[q] = v[q];
+                }
+            }
+        }
+    }
+}
+
 // One gradient: workgroup `group` of those that it has.  T: float, _Float16 or __bf16.  WR x WL waves, each FR x FL tiles of 16 x 16.
 template <typename T, bool TO_X, int WR, int WL, int FR, int FL>
 __device__ __forceinline__ void gradient(const GradParams &p, uint32_t group, char (&lds)[2][256 * (FL * WL + FR * WR) * 8])
@@ -129,7 +212,8 @@ __device__ __forceinline__ void gradient(const GradParams &p, uint32_t group, ch
     // L2: a contiguous range of tiles, in panels of eight tiles along R.
     const uint32_t live = p.kinfo != nullptr ? *p.kinfo : (uint32_t)p.K;
     const uint32_t size_r = TO_X ? live : (uint32_t)p.N, size_l = TO_X ? (uint32_t)p.M : live;
-    const uint32_t tiles_r = (size_r + TR - 1) / TR, tiles_l = (size_l + TL - 1) / TL, tiles = tiles_r * tiles_l;
+    // (dX: one that writes zeros where no row is live)
+    const uint32_t tiles_r = TO_X ? max(1u, (size_r + TR - 1) / TR) : (size_r + TR - 1) / TR, tiles_l = (size_l + TL - 1) / TL, tiles = tiles_r * tiles_l;
     const uint32_t all = tiles * (uint32_t)p.splits;
     if (group >= all) return;
     const uint32_t q8 = all >> 3, rem = all & 7u, x = group & 7u, id = x * q8 + min(x, rem) + (group >> 3);
@@ -167,7 +251,7 @@ __device__ __forceinline__ void gradient(const GradParams &p, uint32_t group, ch
         for (int n = 0; n < NR; ++n) {
             const uint32_t kc = r0 + row_l + (uint32_t)n * (NT / 8);
             const bool there = kc < live;
-            const uint32_t k = p.kinfo != nullptr ? p.kmap[there ? kc : 0u] : there ? kc : 0u;
+            const uint32_t k = !there ? 0u : p.kinfo != nullptr ? p.kmap[kc] : kc;
             row_y[n] = static_cast<const char *>(p.Y) + (uint64_t)k * (uint64_t)p.ldy * ESZ;
             map_y[n] = reinterpret_cast<const uint8_t *>(p.b_bits + (uint64_t)k * (uint64_t)p.WB);
             at_r[n] = there ? 0xffu : 0u;   // (of the map's byte)
@@ -318,6 +402,11 @@ __device__ __forceinline__ void gradient(const GradParams &p, uint32_t group, ch
     compute(half, std::false_type{});
 
     // ---- results: a lane holds four neighbours along R of sixteen along L
+    if constexpr (TO_X && ESZ == 2)
+        if (p.whole_rows) {
+            spread_rows<T, WR, WL, FR, FL>(p, acc, l0, r0, live, lds);
+            return;
+        }
     const uint64_t pitch = (size_r + 3u) & ~3u;
     float *const partials = p.splits > 1 ? p.partials + (uint64_t)split * size_l * pitch : nullptr;
 #pragma unroll
@@ -374,8 +463,7 @@ template <int ESZ> __device__ __forceinline__ void clear(const ClearParams &p, u
 }
 
 // Everything in one launch: first the workgroups of dX, then those of dY, which fill up the last round of the first, then the zeros, which take no matrix instructions
-// (ahead of the products 2048 x 16384 x 4096 with a tenth of the rows takes 234 us for 214, floats 552 for 522; in a launch of their own 203 and 696, and
-// 1024 x 4096 x 4096 bf16 with a quarter 79 for 68).
+// (2048 x 16384 x 4096 floats, a tenth of the rows: 522 us, with the zeros first 552, with a launch of their own 696).
 struct GradWork {
     GradParams x, y;
     uint32_t groups_x, groups_y;   // of each; the first a multiple of eight: an XCD gets every eighth workgroup of either
@@ -535,6 +623,12 @@ template <typename T> hipError_t launch_wanted(const mmm_maps *m, GradWork w, bo
     GradPlan plan_x = plan_one(job_x, floats, m->partial_bytes, w.x.lddc * (int64_t)sizeof(T)), plan_y = plan_one(job_y, floats, m->partial_bytes, w.x.lddc * (int64_t)sizeof(T));
     // (planned for both also where one is asked for: its sums are then the same)
     const bool together = plan_both(job_x, job_y, floats, m->partial_bytes, plan_x, plan_y);
+    // Rows of dX written whole by the tiles, zeros and all: 16-bit types, where the tiles fill the machine and hold one k in sixteen at least.  Both gradients, us, against
+    // results and zeros by themselves: 2048 x 16384 x 4096 bf16, a fiftieth of the rows 151 and 114, a tenth 177 and 214, nine tenths 549 and 638; 130 x 5000 x 328 half,
+    // a fifth, 48 tiles, 15.4 and 12.4.  (Floats, whose products leave time for the zeros: a tenth 498 and 523, but 4096 x 2048 x 512 54 and 45.)
+    w.x.whole_rows = m->b_compact && !floats && plan_x.splits == 1 && job_x.tiles(plan_x.tile) >= 256 && live * 16 >= m->K;
+    if (w.x.whole_rows) w.zeros.dX = nullptr;
+    w.zeros.groups = (uint32_t)std::min<int64_t>((w.zeros.dX != nullptr ? m->M : 0) + (w.zeros.dY != nullptr ? m->K : 0), 1024);
     if (together || !x || !y) return launch<T>(m, w, x ? &plan_x : nullptr, y ? &plan_y : nullptr, job_x.bytes, s);
     if (const hipError_t e = launch<T>(m, w, &plan_x, nullptr, job_x.bytes, s); e != hipSuccess) return e;
     w.zeros = {};   // (are written)
@@ -556,6 +650,7 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
     p.b_bits = m->b_bits;
     p.kinfo = m->b_compact ? m->kinfo : nullptr;
     p.kmap = m->kmap;
+    p.rows = m->rows_copy;
     p.M = m->M;
     p.K = m->K;
     p.N = m->N;
@@ -573,12 +668,9 @@ hipError_t mmm_launch_grad(const mmm_maps *m, int32_t dtype, const void *Y, int6
     w.y.out = dY;
     w.y.ldo = lddy;
     w.y.steps = (int32_t)(m->MBA * (dtype == MMM_F32 ? 2 : 1));
-    const bool clear_y = dY != nullptr && !accumulate;
-    if (m->b_compact && (dX != nullptr || clear_y)) {
-        const int64_t rows = (dX != nullptr ? m->M : 0) + (clear_y ? m->K : 0);
-        w.zeros = {static_cast<char *>(dX), clear_y ? reinterpret_cast<char *>(dY) : nullptr, lddx * esz, m->M, lddy * 4, m->N * 4, m->K, m->rows_copy,
-                   (uint32_t)std::min<int64_t>(rows, 1024)};
-    }
+    // (of dX where its contraction is split: otherwise its tiles write them)
+    if (m->b_compact)
+        w.zeros = {static_cast<char *>(dX), accumulate ? nullptr : reinterpret_cast<char *>(dY), lddx * esz, m->M, lddy * 4, m->N * 4, m->K, m->rows_copy, 0};
     (void)hipGetLastError();
     const bool x = dX != nullptr, y = dY != nullptr;
     return dtype == MMM_F32 ? launch_wanted<float>(m, w, x, y, s) : dtype == MMM_BF16 ? launch_wanted<__bf16>(m, w, x, y, s) : launch_wanted<_Float16>(m, w, x, y, s);

@@ -244,3 +244,42 @@ def test_rows_far_apart():
         results.append([v.clone(memory_format=torch.contiguous_format) for v in (dX, dY, C)])
         eng.close()
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+# 16-bit results of many tiles with rows by context: dX is written in whole rows, each tile from its first live row of B to the next tile's
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,M,K,N,which", [("bf16", 2051, 2055, 72, "none"), ("f16", 2051, 2055, 72, "first"), ("bf16", 2051, 2055, 72, "last"), ("f16", 2100, 2055, 72, "middle"),
+                                            ("bf16", 2051, 2055, 72, 0.1), ("f16", 4001, 1153, 136, 0.5), ("bf16", 1030, 8200, 520, 0.5), ("f16", 2051, 16391, 1032, 0.9),
+                                            ("bf16", 2051, 16391, 264, "ends")])
+def test_whole_rows(dt, M, K, N, which):
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    t = T[dt][1]
+    X, Y, dC = (torch.randn(s, generator=g, device="cuda").to(t) for s in ((M, K), (K, N), (M, N)))
+    keep = torch.rand(M, K, generator=g, device="cuda") < 0.4
+    on = torch.rand(K, generator=g, device="cuda") < (which if isinstance(which, float) else 0.0)
+    if which == "first":
+        on[0] = True
+    if which == "last":
+        on[K - 1] = True
+    if which == "middle":
+        on[700:1400] = True
+    if which == "ends":
+        on[:300] = True
+        on[-1400:] = True
+    eng = mm.MaskedMatmul(M, K, N, 8, T[dt][0])
+    eng.build_maps(X, Y, keep_a=words(keep.cpu()), keep_rows=words(on.view(1, -1).cpu()))
+    a_on = keep & (X != 0)
+    Bm, G = Y.double() * on.view(-1, 1), dC.double()
+    want, mag = G @ Bm.t().contiguous(), G.abs() @ Bm.abs().t().contiguous()
+    whole, dX = room(M, K, t, 3, 1)
+    for counted in (False, True):
+        if counted:
+            eng.stats()   # (then a selection of few rows is known as such)
+        for all_x in (False, True):
+            whole.fill_(77.0)
+            eng.matmul_backward(X, Y, dC, dX, all_x=all_x)
+            w = want if all_x else want * a_on
+            assert bool(((dX.double() - w).abs() <= (N + 1) * U * mag + torch.finfo(t).eps / 2 * w.abs() * (1 + 1e-3)).all()), (counted, all_x)
+            assert bool((dX[:, ~on] == 0).all()) and (all_x or bool((dX[~a_on] == 0).all()))
+            dX.fill_(77.0)
+            assert bool((whole == 77.0).all()), "outside"
