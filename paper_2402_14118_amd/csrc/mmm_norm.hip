@@ -11,7 +11,7 @@
 //     d_x = r (d - x^ mean(d x^) - mean(d))                 (the last only with a mean)
 //     d_w = sum over rows of d_n x^,  d_b = sum over rows of d_n
 // mean, r and x^ are made again from the row, which has to be read for x^ anyway: nothing is kept from the forward call.  A workgroup takes rows
-// i, i + G, ... and keeps the sums over rows of its columns in registers; the G partial sums are added by a second launch,
+// i, i + G, ... (or some of each turn) and keeps the sums over rows of its columns in registers; the G partial sums are added by a second launch,
 // in order, so results do not depend on which workgroup ends first.
 #include <algorithm>
 #include <type_traits>
@@ -65,6 +65,37 @@ template <int VALUES, int WAVES> __device__ __forceinline__ void add_over_row(fl
         v[q] = sum;
     }
 }
+// The same for a workgroup of several rows side by side, WPR waves each: those from wave `first` on.  A row of one wave needs no room, and no barrier.
+template <int VALUES, int WPR, int ALL> __device__ __forceinline__ void add_over_rows(float (&v)[VALUES], float (*room)[ALL], int first)
+{
+    typedef float vec __attribute__((ext_vector_type(WPR < 4 ? 2 : 4)));
+    constexpr int PER = WPR < 4 ? 2 : 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int q = 0; q < VALUES; ++q) v[q] = add_over_lanes(v[q]);
+    if constexpr (WPR == 1) {
+#pragma unroll
+        for (int q = 0; q < VALUES; ++q) v[q] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[q]), 63));
+    } else {
+        if (lane == 63)
+#pragma unroll
+            for (int q = 0; q < VALUES; ++q) room[q][wave] = v[q];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < VALUES; ++q) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WPR; w += PER) {
+                const vec some = *reinterpret_cast<const vec *>(&room[q][first + w]);
+                if constexpr (PER == 2)
+                    sum += some.x + some.y;
+                else
+                    sum += (some.x + some.y) + (some.z + some.w);
+            }
+            v[q] = sum;
+        }
+    }
+}
 template <int N> __device__ __forceinline__ void clear_rooms(float *rooms)
 {
     for (int q = threadIdx.x; q < N; q += blockDim.x) rooms[q] = 0.f;
@@ -80,14 +111,15 @@ template <int N> __device__ __forceinline__ void clear_rooms(float *rooms)
 enum RowKind { EVEN, ODD, SHORT };
 template <RowKind KIND, int V> struct Pieces {
     int at[V], first[V], count[V];   // where piece i is read; its elements that are this lane's: first, and how many
-    __device__ __forceinline__ explicit Pieces(int N)
+    // lane `tid` of the `width` that a row has
+    __device__ __forceinline__ Pieces(int N, int tid, int width)
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int col = (i * (int)blockDim.x + (int)threadIdx.x) * PIECE;
+            const int col = (i * width + tid) * PIECE;
             at[i] = KIND == SHORT ? 0 : min(col, N - PIECE);
             first[i] = KIND == SHORT ? 0 : min(col - at[i], PIECE);
-            count[i] = KIND == SHORT ? threadIdx.x == 0 ? N : 0 : PIECE - first[i];
+            count[i] = KIND == SHORT ? tid == 0 ? N : 0 : PIECE - first[i];
         }
     }
     __device__ __forceinline__ bool on(int i) const { return KIND != EVEN || first[i] == 0; }
@@ -137,7 +169,7 @@ template <typename T, typename TH, typename TY, int V, int WAVES, RowKind KIND> 
 {
     __shared__ __align__(16) float rooms[2][4][1][WAVES];   // (rows in turn: of a row, a wave may still read what another has gone past)
     clear_rooms<2 * 4 * WAVES>(&rooms[0][0][0][0]);
-    const Pieces<KIND, V> mine((int)p.d.N);
+    const Pieces<KIND, V> mine((int)p.d.N, (int)threadIdx.x, (int)blockDim.x);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < p.d.M; row += gridDim.x, turn ^= 1) {
         float h[V][PIECE], v[V][PIECE];
@@ -269,14 +301,20 @@ template <typename T, int V, RowKind KIND> struct GradColumns {
     }
 };
 
+// Rows side by side in a workgroup, of WPR waves each
+constexpr int rows_beside(int wpr) { return wpr >= 8 ? 1 : 8 / wpr; }
 // BIASES: the norm behind the block has a bias, or sums for biases are asked for
-template <typename T, typename TH, typename TY, int V, int WAVES, bool BIASES, RowKind KIND>
-__global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const NormGradParams p)
+template <typename T, typename TH, typename TY, int V, int WPR, bool BIASES, RowKind KIND>
+__global__ __launch_bounds__(64 * WPR * rows_beside(WPR)) void mmm_block_norm_grad_kernel(const NormGradParams p)
 {
+    constexpr int SIDE = rows_beside(WPR), WAVES = WPR * SIDE;
     __shared__ __align__(16) float rooms[2][4][3][WAVES];   // (rows in turn, as above)
+    __shared__ float fold[SIDE > 1 ? SIDE - 1 : 1][SIDE > 1 ? V * PIECE : 1][64 * WPR];
     clear_rooms<2 * 4 * 3 * WAVES>(&rooms[0][0][0][0]);
     const mmm_block_norm_grads &g = p.g;
-    const Pieces<KIND, V> mine((int)p.d.N);
+    const int beside = SIDE > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / (64 * WPR)) : 0, first = beside * WPR;   // which of the rows side by side
+    const int tid = (int)threadIdx.x - beside * 64 * WPR;
+    const Pieces<KIND, V> mine((int)p.d.N, tid, SIDE > 1 ? 64 * WPR : (int)blockDim.x);
     const bool pre = p.d.pre != MMM_NORM_NONE, block = p.block, post = p.d.post != MMM_NORM_NONE;
     const bool pre_mean = p.d.pre == MMM_NORM_LAYER, post_mean = p.d.post == MMM_NORM_LAYER;
     float sums[SUMS][V][PIECE];
@@ -290,9 +328,12 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
     GradColumns<T, V, KIND> columns;
     if (V == 1) columns.load(p, mine, BIASES);   // (wider rows have no registers for them)
     GradRow<T, TH, TY, V, KIND> next;
-    next.load(p, mine, blockIdx.x);   // (there are no more workgroups than rows)
+    next.load(p, mine, min((int64_t)blockIdx.x * SIDE + beside, p.d.M - 1));
     int turn = 0;
-    for (int64_t row = blockIdx.x; row < p.d.M; row += gridDim.x, turn ^= 1) {
+    for (int64_t row0 = (int64_t)blockIdx.x * SIDE; row0 < p.d.M; row0 += (int64_t)gridDim.x * SIDE, turn ^= 1) {
+        // (behind the last row: that one again, with gradients of zero, and nothing is stored)
+        const bool there = SIDE == 1 || row0 + beside < p.d.M;
+        const int64_t row = there ? row0 + beside : p.d.M - 1;
         float x[V][PIECE], dn[V][PIECE], d[V][PIECE], y[V][PIECE], gate[V][PIECE];
         const float row_gate = p.d.gate == MMM_GATE_ROW ? (float)static_cast<const T *>(p.row_gates)[row] : 1.f;
 #pragma unroll
@@ -303,13 +344,13 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
             for (int q = 0; q < PIECE; ++q) {   // (zeros for what is another lane's; of operands that are not there nothing is used)
                 const bool on = mine.mine(i, q);
                 x[i][q] = on ? (float)next.x[i][q] : 0.f;
-                dn[i][q] = on ? (float)next.dn[i][q] : 0.f;
-                d[i][q] = p.has_d_h_out && on ? (float)next.d[i][q] : 0.f;
+                dn[i][q] = on && there ? (float)next.dn[i][q] : 0.f;
+                d[i][q] = p.has_d_h_out && on && there ? (float)next.d[i][q] : 0.f;
                 y[i][q] = on ? (float)next.y[i][q] : 0.f;
             }
         }
         if (V > 1) columns.load(p, mine, BIASES);
-        next.load(p, mine, min(row + (int64_t)gridDim.x, p.d.M - 1));
+        next.load(p, mine, min(row0 + (int64_t)gridDim.x * SIDE + beside, p.d.M - 1));
         // both rows standardised together: one sum for means, one for variances
         float s2[2] = {0.f, 0.f};
         if (pre_mean || post_mean) {
@@ -321,7 +362,7 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
                         s2[0] += x[i][q];
                         s2[1] += y[i][q];
                     }
-            add_over_row(s2, rooms[turn][0]);
+            add_over_rows<sizeof(s2) / sizeof(float), WPR, WAVES>(s2, rooms[turn][0], first);
             const float mx = pre_mean ? s2[0] * p.inv_n : 0.f, my = post_mean ? s2[1] * p.inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -341,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
                     s2[0] += x[i][q] * x[i][q];
                     s2[1] += y[i][q] * y[i][q];
                 }
-        add_over_row(s2, rooms[turn][1]);
+        add_over_rows<sizeof(s2) / sizeof(float), WPR, WAVES>(s2, rooms[turn][1], first);
         const float rx = 1.f / sqrtf(s2[0] * p.inv_n + p.d.eps), ry = post ? 1.f / sqrtf(s2[1] * p.inv_n + p.d.eps) : 1.f;
         // through the norm in front of the next block: d becomes the gradient of h'
         if (pre) {
@@ -359,7 +400,7 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
                     c[1] += dn[i][q];
                 }
             }
-            add_over_row(c, rooms[turn][2]);
+            add_over_rows<sizeof(c) / sizeof(float), WPR, WAVES>(c, rooms[turn][2], first);
             const float along = c[0] * p.inv_n, mean = pre_mean ? c[1] * p.inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -367,7 +408,7 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
 #pragma unroll
                     for (int q = 0; q < PIECE; ++q) d[i][q] += rx * (dn[i][q] - x[i][q] * along - mean);
         }
-        if (g.d_h != nullptr) {
+        if (g.d_h != nullptr && there) {
             const float alpha = block ? p.d.alpha : 1.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -400,11 +441,11 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
                 c[0] += d[i][q] * y[i][q];
                 c[1] += d[i][q];
             }
-            if (p.d.gate == MMM_GATE_FULL && g.d_gate != nullptr) mine.store(static_cast<T *>(g.d_gate) + row * g.ldd_gate, i, dgate);
+            if (p.d.gate == MMM_GATE_FULL && g.d_gate != nullptr && there) mine.store(static_cast<T *>(g.d_gate) + row * g.ldd_gate, i, dgate);
         }
-        add_over_row(c, rooms[turn][3]);
-        if (p.d.gate == MMM_GATE_ROW && g.d_gate != nullptr && threadIdx.x == 0) static_cast<float *>(g.d_gate)[row] = c[2];
-        if (g.d_y != nullptr) {
+        add_over_rows<sizeof(c) / sizeof(float), WPR, WAVES>(c, rooms[turn][3], first);
+        if (p.d.gate == MMM_GATE_ROW && g.d_gate != nullptr && there && tid == 0) static_cast<float *>(g.d_gate)[row] = c[2];
+        if (g.d_y != nullptr && there) {
             const float along = post ? c[0] * p.inv_n : 0.f, mean = post_mean ? c[1] * p.inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -419,6 +460,22 @@ __global__ __launch_bounds__(64 * WAVES) void mmm_block_norm_grad_kernel(const N
 #pragma unroll
     for (int s = 0; s < SUMS; ++s) {
         if (p.place[s] < 0) continue;
+        if constexpr (SIDE > 1) {   // the rows side by side, in order
+            __syncthreads();
+            if (beside > 0)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int q = 0; q < PIECE; ++q) fold[beside - 1][i * PIECE + q][tid] = sums[s][i][q];
+            __syncthreads();
+            if (beside > 0) continue;
+#pragma unroll
+            for (int b = 0; b < SIDE - 1; ++b)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int q = 0; q < PIECE; ++q) sums[s][i][q] += fold[b][i * PIECE + q][tid];
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (mine.on(i)) mine.store(p.partials + ((int64_t)blockIdx.x * p.sums + p.place[s]) * p.d.N, i, sums[s][i]);
@@ -540,12 +597,24 @@ template <typename F> auto with_types(const mmm_block_norm_desc &d, F f)
     return with_stream_types<float>(d, f);
 }
 
+// Waves for a row of the gradients, and pieces per lane.  Rows of whole pieces of up to 2048 elements stand side by side in a workgroup of eight waves (2, 4 or 8): they share
+// its barriers, a row of one wave needs none, and partial sums are fewer (2048 x 512 half beside float, with biases, 29 -> 12 us; 8192 x 1024 bf16 32 -> 26;
+// 777 x 1992 floats 19.8 -> 18.1; 4096 wide in two pieces per lane, two rows beside each other, has no registers for the columns: 29 -> 31).
+struct GradShape { uint32_t threads; int pieces, waves, beside; };
+GradShape grad_shape(int64_t N)
+{
+    const RowShape r = row_shape(N);
+    if (N >= PIECE && (N % PIECE != 0 || N > 2048)) return {r.threads, r.pieces, r.pieces == 4 ? 16 : 8, 1};
+    const int waves = N <= 512 ? 1 : N <= 1024 ? 2 : 4;
+    return {512, 1, waves, rows_beside(waves)};
+}
 // Workgroups of the gradients: as many as the registers of the chip hold at a time (8 waves on a compute unit), so that partial sums are few, and
-// all with the same number of rows but for one.  2048 x 4096 bf16, before EVEN: 256 groups 28.6 us and 4.0 for adding up, 512 32.3 and 5.5, 1024 38.8 and 8.3.
+// all with the same number of turns but for one.  2048 x 4096 bf16, an older form: 256 groups 28.6 us and 4.0 for adding up, 512 32.3 and 5.5, 1024 38.8 and 8.3.
 int64_t norm_grad_groups(int64_t M, int64_t N)
 {
-    const int64_t slots = 256 * std::max<int64_t>(1, 512 / row_shape(N).threads), rows = (M + slots - 1) / slots;
-    return (M + rows - 1) / rows;
+    const GradShape shape = grad_shape(N);
+    const int64_t slots = 256 * (shape.beside > 1 ? 1 : std::max<int64_t>(1, 512 / shape.threads)), turns = (M + shape.beside - 1) / shape.beside, each = (turns + slots - 1) / slots;
+    return (turns + each - 1) / each;
 }
 int64_t act_strips(int64_t N) { return (N + ACT_COLS - 1) / ACT_COLS; }
 int64_t act_shares(int64_t M, int64_t N)
@@ -595,7 +664,7 @@ size_t mmm_block_norm_grad_bytes(int64_t M, int64_t N) { return (size_t)norm_gra
 hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_block_norm_grads &g, void *workspace, hipStream_t s)
 {
     if (d.M < 1 || d.N < 1 || d.N > MMM_NORM_MAX_WIDTH) return hipErrorInvalidValue;
-    const RowShape shape = row_shape(d.N);
+    const GradShape shape = grad_shape(d.N);
     NormGradParams p{d, g, 1.f / (float)d.N, static_cast<float *>(workspace), {}, 0, g.gate_values, g.d_h_out != nullptr, d.gate >= MMM_GATE_COL, g.post_weight != nullptr,
                      g.post_bias != nullptr, g.pre_weight != nullptr, g.y != nullptr};
     // What is not there is read from what is: h' and d_n with a norm in front, else d_h' and y (the types of a block that is not there are
@@ -632,12 +701,23 @@ hipError_t mmm_launch_block_norm_grad(const mmm_block_norm_desc &d, const mmm_bl
         typedef decltype(th) TH;
         typedef decltype(ty) TY;
         const bool biases = g.d_pre_bias != nullptr || g.d_post_bias != nullptr || g.post_bias != nullptr;
-        void (*fn)(const NormGradParams) = d.N < PIECE         ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 4, true, SHORT>
-                                           : shape.pieces == 2 ? mmm_block_norm_grad_kernel<T, TH, TY, 2, 8, true, ODD>
-                                           : shape.pieces == 4 ? mmm_block_norm_grad_kernel<T, TH, TY, 4, 16, true, ODD>
-                                           : d.N % PIECE != 0  ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, ODD>
-                                           : biases            ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, EVEN>
-                                                               : mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, false, EVEN>;
+        void (*fn)(const NormGradParams);
+        if (d.N < PIECE)
+            fn = mmm_block_norm_grad_kernel<T, TH, TY, 1, 1, true, SHORT>;
+        else if (shape.pieces == 4)
+            fn = mmm_block_norm_grad_kernel<T, TH, TY, 4, 16, true, ODD>;
+        else if (shape.pieces == 2)
+            fn = mmm_block_norm_grad_kernel<T, TH, TY, 2, 8, true, ODD>;
+        else if (d.N % PIECE != 0)
+            fn = mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, ODD>;
+        else if (shape.waves == 1)
+            fn = biases ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 1, true, EVEN> : mmm_block_norm_grad_kernel<T, TH, TY, 1, 1, false, EVEN>;
+        else if (shape.waves == 2)
+            fn = biases ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 2, true, EVEN> : mmm_block_norm_grad_kernel<T, TH, TY, 1, 2, false, EVEN>;
+        else if (shape.waves == 4)
+            fn = biases ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 4, true, EVEN> : mmm_block_norm_grad_kernel<T, TH, TY, 1, 4, false, EVEN>;
+        else
+            fn = biases ? mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, true, EVEN> : mmm_block_norm_grad_kernel<T, TH, TY, 1, 8, false, EVEN>;
         hipLaunchKernelGGL(fn, dim3((uint32_t)groups), dim3(shape.threads), 0, s, p);
         return 0;
     });

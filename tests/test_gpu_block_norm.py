@@ -394,3 +394,20 @@ def test_more_elements_than_32_bits_count():
         assert torch.equal(dbias, ends[1].float().clamp(min=0).sum(0) + (rows - tail))
         results.append(parts + [to[-tail:].clone()])
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+# several rows side by side in a workgroup: fewer rows than that, some left over, more than one turn
+@pytest.mark.gpu
+@pytest.mark.parametrize("args", [(1, 512, "bf16", "bf16", "bf16", "rms", "rms", "col", 0, "weight"), (5, 8, "f32", "f32", "f32", "layer", "rms", "full", 1, "both"),
+                                  (13, 1024, "f16", "f32", "f16", "rms", "layer", "row", 3, "both"), (3, 2048, "bf16", "f32", "f32", "layer", "layer", "none", 0, "weight"),
+                                  (2500, 72, "bf16", "bf16", "bf16", "rms", "rms", "col", 0, "weight"), (1541, 640, "f32", "f32", "f32", "rms", "rms", "full", 0, "weight"),
+                                  (1031, 1032, "f16", "f16", "f32", "layer", "none", "row", 8, "both")], ids=lambda a: "-".join(map(str, a)))
+def test_rows_side_by_side(args):
+    c = Case(*args)
+    want = c.backward()
+    got = c.run_backward(list(want))
+    for k, (w, mag) in want.items():
+        check(got[k], w, mag, k)
+        c.untouched(got[k])
+    again = c.run_backward(list(want))
+    assert all(torch.equal(got[k], again[k]) for k in want)
