@@ -404,7 +404,7 @@ mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype o
  * X must be the one the A side was built from (address, ldx); the Y given is what is read, under the maps as built.
  * Masked-out elements of X and unoccupied blocks of Y never reach the arithmetic, whatever they hold.  Elements of dC are expected
  * to be finite: one that is not makes row i of dX and column j of dY non-finite, or less than that.
- * Sums in float, in an order that depends on the shape, the form of the maps and the counts of mmm_maps_stats only.  Partial sums of a split contraction lie in
+ * Sums in float, in an order that depends on the shape, lddc, the form of the maps and the counts of mmm_maps_stats only (not on which of the two is asked for).  Partial sums of a split contraction lie in
  * the workspace of the maps, as mmm_matmul's: two calls on one handle that may run at the same time race.
  * Errors: MMM_ERR_INVALID_ARG, MMM_ERR_SHAPE (also: a leading dimension of 2^22 and more), MMM_ERR_DTYPE (doubles; misaligned pointer), MMM_ERR_MAPS_MISMATCH (as
  * mmm_matmul), MMM_ERR_DEVICE. */
