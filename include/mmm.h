@@ -372,8 +372,8 @@ typedef struct {
 
 /* C = act(A x B + bias) + residual.  With ma == NULL the product is that of mmm_matmul, and everything said there about X, Y and the
  * maps holds; with ma it is that of mmm_matmul_fused (the mask evaluated inside the multiplication; only the B side of the maps is
- * used; meant for few rows with many zeros: a dense X is multiplied faster by MMM_PATH_MATRIX, from maps).  The sums are those of these calls: kernel, plan and order are the same, so that C rounded to
- * float is theirs bit by bit where nothing is done in the epilogue.  Rows of A and columns of B without any product give act(bias) + residual.
+ * used; meant for few rows with many zeros: a dense X is multiplied faster by MMM_PATH_MATRIX, from maps).
+ * The sums are those of these calls: kernel, plan and order are the same, so that C rounded to float is theirs bit by bit where nothing is done in the epilogue.  Rows of A and columns of B without any product give act(bias) + residual.
  * The activation and all that follows are computed in the type of the sums, whatever out_dtype is.
  * Partial sums of a split K lie in the workspace of the maps, as mmm_matmul's: two calls on one handle that may run at the same time race.
  * Errors: MMM_ERR_INVALID_ARG (NULL pointer, unknown activation, bad mask), MMM_ERR_SHAPE (a leading dimension too small),
@@ -404,8 +404,8 @@ mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype o
  * X must be the one the A side was built from (address, ldx); the Y given is what is read, under the maps as built.
  * Masked-out elements of X and unoccupied blocks of Y never reach the arithmetic, whatever they hold.  Elements of dC are expected
  * to be finite: one that is not makes row i of dX and column j of dY non-finite, or less than that.
- * Sums in float, in an order that depends on the shape, lddc, the form of the maps and the counts of mmm_maps_stats only (not on which of the two is asked for).  Partial sums of a split contraction lie in
- * the workspace of the maps, as mmm_matmul's: two calls on one handle that may run at the same time race.
+ * Sums in float, in an order that depends on the shape, lddc, the form of the maps and the counts of mmm_maps_stats only
+ * (not on which of the two is asked for).  Partial sums of a split contraction lie in the workspace of the maps, as mmm_matmul's: two calls on one handle that may run at the same time race.
  * Errors: MMM_ERR_INVALID_ARG, MMM_ERR_SHAPE (also: a leading dimension of 2^22 and more), MMM_ERR_DTYPE (doubles; misaligned pointer), MMM_ERR_MAPS_MISMATCH (as
  * mmm_matmul), MMM_ERR_DEVICE. */
 mmm_status mmm_matmul_backward(const mmm_maps *maps, mmm_dtype dt, const void *X, int64_t ldx, const void *Y, int64_t ldy,

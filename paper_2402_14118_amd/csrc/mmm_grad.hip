@@ -13,8 +13,8 @@
 // A comes from the image that the builder made, masked, compacted and with 16 (floats: 4) rows of a column side by side, which is the
 // order that an operand of dY wants.  dC is read row by row there, and turned by ds_read_b64_tr_b16 (floats: one by one) on the way out of LDS.
 // Operands wait in registers while the step before is multiplied, and are laid into the other half of LDS between its last products: masks are applied on the
-// way, one barrier per step (placed behind the products instead: 2048 x 16384 x 4096 bf16, both gradients, 612 us for 565).  In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that
-// eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
+// way, one barrier per step (placed behind the products instead: 2048 x 16384 x 4096 bf16, both gradients, 612 us for 565).
+// In LDS an operand row is 128 bytes, its eight 16-byte pieces turned with the row, so that eight rows' pieces lie in different banks; rows of dC in dY have their 32 (floats: 64) byte pieces turned.
 //
 // What bounds it.  Large results: the matrix cores at the clock that the power limit leaves (4096^3 half 1096 TFLOP/s for both, where a library product
 // of 8192^3 bf16 reaches 1140; 2048 x 16384 x 4096 bf16 973; floats 135 of 155).  Small ones: the steps of a workgroup, one after another, and one to four
