@@ -150,6 +150,10 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
     constexpr uint32_t ESZ = (uint32_t)sizeof(T);
     constexpr int C16 = 16 / (int)ESZ;         // columns per lane = entries of a list per load
     constexpr int LPR = BW / C16;              // lanes per entry
+    // Eight loads in flight, else four.  They take 3 to 30 vector registers more: few rows have no other waves for these (1 x 8, 2 x 8: 8 x 4096 x 4096 doubles 7.4 -> 6.7 us,
+    // 1 x 11740 x 328 floats, all on, 340 -> 310, others .97 to 1.01), more rows do (8 x 1: 2048^3 floats, a tenth, 45.6 -> 59.6; 8 x 2: 100 x 4096 x 4096 floats 32.7 -> 34.6;
+    // 4 x 4: 16 x 8192 x 4096 half 45.7 -> 48.2; .96 to .99 at best).
+    constexpr bool DEEP = FUSED && KS == 8;
     typedef typename Elem<T>::acc acc_t;
     typedef typename Elem<T>::pattern pattern;
     typedef typename Row16<(int)ESZ>::type row16;
@@ -379,7 +383,8 @@ __global__ __launch_bounds__(CW *KS * 64) __attribute__((amdgpu_waves_per_eu(FUS
                 };
                 uint32_t t = 0;
                 if (FUSED) {
-                    for (; t + 6 * C16 < rmax; t += 8 * C16) batch(t, std::integral_constant<int, 8>{});
+                    if (DEEP)
+                        for (; t + 6 * C16 < rmax; t += 8 * C16) batch(t, std::integral_constant<int, 8>{});
                     for (; t + 2 * C16 < rmax; t += 4 * C16) batch(t, std::integral_constant<int, 4>{});
                 }
                 for (; t + C16 < rmax; t += 2 * C16) batch(t, std::integral_constant<int, 2>{});
@@ -496,7 +501,7 @@ static hipError_t launch_pairs(const mmm_maps *m, int32_t dtype, const void *X, 
     // the decode shape), fewer columns per workgroup and K shared out over several waves, unless there is next to nothing of it.
     // With the mask evaluated here every column span repeats the predicate, so the spans are as wide as leaves every compute unit a
     // workgroup (4 x 16384 x 4096 bf16: 64, 128, 256 columns: 6.6, 7.1, 8.0 us back to back; 8 x 8192 x 2048 floats: 64, 128: 10.5, 13.8; 1 x 11740 x 328 floats, all
-    // elements on: 23, 41; 16 x 8192 x 4096 bf16, where 128 make two rounds: 8.7, 256: 5.6).  Columns do not change the order of a sum.
+    // elements and a tenth of the blocks on: 18, 27; 16 x 8192 x 4096 bf16, where 128 make two rounds: 8.7, 256: 5.6).  Columns do not change the order of a sum.
     const int64_t wide = (m->N + 511) / 512 * m->M;
     PairsShape sh{8, 1, 64};
     if (wide < 1024 && (fused || m->WA > 32)) {
