@@ -255,7 +255,7 @@ mmm_status mmm_maps_stats(const mmm_maps *maps, uint64_t *nnz_a, uint64_t *occup
  * of a single product, else rounded once, is off by up to 2.1 instead of 1 times 2^-24 of it.  Blocks with an element that parts do not hold (magnitudes of 2^55 and more or
  * below 2^-110, infinities, NaN) are multiplied as floats behind the others, up to seven times slower where all have one:
  * floats are left as they are where mmm_maps_stats has counted more than a few.  mmm_build_maps lays the operands out for one or the other; a side that is
- * built alone takes the form of the side that is kept, and a build or multiplication that is captured into a graph fixes the handle's form
+ * built alone takes the form of the side that is kept, and a build, a multiplication or a gradient dY (mmm_matmul_backward) that is captured into a graph fixes the handle's form
  * for as long as the graph, or what has been cloned or instantiated from it, exists (a graph that an executable one is updated from
  * has to be kept by the caller as long as that one).
  * Products the maps skip contribute exactly 0, whatever the skipped operands

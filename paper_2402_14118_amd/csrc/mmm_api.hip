@@ -1070,6 +1070,8 @@ mmm_status mmm_matmul_backward(const mmm_maps *maps, mmm_dtype dt, const void *X
     if (!placed(X, dt) || !placed(Y, dt) || !placed(dC, dt) || !placed(dX, dt) || !placed(dY, MMM_F32)) return MMM_ERR_DTYPE;
     if (!maps->a_built || !maps->b_built || maps->a_dtype != dt || maps->b_dtype != dt) return MMM_ERR_MAPS_MISMATCH;
     if (maps->a_src != X || maps->a_src_ld != ldx) return MMM_ERR_MAPS_MISMATCH;   // the values of A are those of the image
+    // (dX does not read the image)
+    if (dY != nullptr && form_is_captured(maps, dt, static_cast<hipStream_t>(hip_stream))) capture_form(maps, maps->a_form, static_cast<hipStream_t>(hip_stream));
     if (hipError_t e = mmm_launch_grad(maps, dt, Y, ldy, dC, lddc, dX, lddx, dY, lddy, accumulate ? 1 : 0, all_x ? 1 : 0, static_cast<hipStream_t>(hip_stream));
         e != hipSuccess) {
         note_device_error("product gradient launch", e);

@@ -283,3 +283,32 @@ def test_whole_rows(dt, M, K, N, which):
             assert bool((dX[:, ~on] == 0).all()) and (all_x or bool((dX[~a_on] == 0).all()))
             dX.fill_(77.0)
             assert bool((whole == 77.0).all()), "outside"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", [0, 1])
+def test_a_captured_gradient_fixes_the_form(form):
+    """dY of a graph reads the image of A as it was laid out when it was captured: builds that follow keep to that, whatever they would choose."""
+    try:
+        mm.mmm_set_option("float_form", form)
+        p = Problem(150, 300, 200, 8, "f32", whole=True)
+        keep, blocks = words(p.a_on), words(p.b_on[:, ::8])
+        p.check(exact=True)
+        want = p.A.t() @ p.G * p.b_on
+        p.dYall.fill_(77.0)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            p.eng.matmul_backward(p.X, p.Y, p.dC, dY=p.dY)
+        mm.mmm_set_option("float_form", 1 - form)
+        p.eng.stats()
+        for _ in range(3):
+            p.eng.build_maps(p.X, p.Y, keep_a=keep, keep_blocks=blocks)
+            assert mm.mmm_matmul_form(p.eng.maps) == form
+            p.dY.fill_(3.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(p.dY.double().cpu(), want)
+            p.check(exact=True)
+    finally:
+        mm.mmm_set_option("float_form", -1)
