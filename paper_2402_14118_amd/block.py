@@ -134,6 +134,7 @@ class MaskedMlp:
     def count(self, stream=None):
         """Count the densities of the last forward call (waits for the stream): what the choice of kernel, of tiles and of the form of floats goes by
         from then on.  Returns ((non-zeros, blocks, products) of the first product, the same of the second; None where its mask is fused)."""
+        check_device(self.device)
         return self.up.stats(stream), None if self.fused else self.down.stats(stream)
 
     def forward(self, N: torch.Tensor, H: torch.Tensor, H_out: torch.Tensor, normed: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
@@ -142,6 +143,7 @@ class MaskedMlp:
         """H_out may be H (backward() does not need H); normed receives n'."""
         if self.W1 is None:
             raise ValueError("set_weights() comes first")
+        check_device(self.device)
         places(self.device, 1, ("N",), N, (self.M, self.width), TORCH_TYPES[self.dtype])
         kept = self.preact if self.training and self.preact is not self.a else None
         self.up.build_maps(N, None, stream=stream)

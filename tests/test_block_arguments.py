@@ -168,3 +168,39 @@ def test_matmul_backward_refuses():
             assert call(**short) == B.MMM_ERR_SHAPE
     finally:
         mm.mmm_maps_release(maps)
+
+
+class Recorder:
+    """Stands for a product: notes what is called."""
+
+    def __init__(self, calls):
+        self.calls = calls
+
+    def __getattr__(self, name):
+        return lambda *args, **kwargs: self.calls.append(name)
+
+
+def mlp_of(calls, M=4, width=16, hidden=32, dtype=mm.MMM_F32, device="cpu", **more):
+    """A holder whose products only note that they were called."""
+    mlp = object.__new__(mm.MaskedMlp)
+    t = torch.float32 if dtype == mm.MMM_F32 else torch.bfloat16
+    room = {name: torch.zeros(M, n, dtype=t) for name, n in (("a", hidden), ("y", width), ("grad_a", hidden), ("grad_y", width))}
+    mlp.__dict__.update(M=M, width=width, hidden=hidden, dtype=dtype, activation=mm.MMM_ACT_RELU, fused=False, training=True, device=torch.device(device),
+                        up=Recorder(calls), down=Recorder(calls), norm=mm.BlockNorm(M, width, dtype, mm.MMM_NORM_RMS, device="cpu", training=True),
+                        preact=room["a"], W1=torch.zeros(width, hidden, dtype=t), W2=torch.zeros(hidden, width, dtype=t), b1=None, b2=None,
+                        workspace=torch.empty(1 << 16, dtype=torch.uint8), **room)
+    mlp.__dict__.update(more)
+    return mlp
+
+
+def test_the_block_refuses_another_current_device_before_any_launch(monkeypatch):
+    """Every product of it would be launched there."""
+    calls = []
+    mlp = mlp_of(calls, device="cuda:1")
+    monkeypatch.setattr(B, "current_device", lambda: 0)
+    monkeypatch.setattr("paper_2402_14118_amd.block.places", lambda *a: (None, 0) * 20)
+    N = torch.zeros(4, 16)
+    for call in (lambda: mlp.forward(N, N, N, N), lambda: mlp.count()):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert calls == []
