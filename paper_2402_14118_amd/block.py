@@ -41,8 +41,8 @@ class BlockNorm:
 
     def forward(self, H: torch.Tensor, normed: Optional[torch.Tensor] = None, H_out: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
                 gate: Optional[torch.Tensor] = None, post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
-                pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
-        """H_out may be H."""
+                pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, stream=None, later: bool = False):
+        """H_out may be H.  later: tensors are checked now, and launch() takes what is returned."""
         t, th, shape, columns = self.type, self.type_h, self.shape, self.columns
         check_device(self.device)
         if gate is not None and self.gate_shape is None:
@@ -50,7 +50,12 @@ class BlockNorm:
         h, ldh, y, ldy, g, ldg, pw, _, pb, _, w, _, b, _, ho, ldho, n, ldn = places(
             self.device, 1, ("H", "Y", "gate", "post_weight", "post_bias", "pre_weight", "pre_bias", "H_out", "normed"), H, shape, th, Y, shape, self.type_y,
             gate, self.gate_shape, t, post_weight, columns, t, post_bias, columns, t, pre_weight, columns, t, pre_bias, columns, t, H_out, shape, th, normed, shape, t)
+        if later:
+            return h, ldh, y, ldy, g, ldg, pw, pb, w, b, ho, ldho, n, ldn
         B._check(B.native.block_norm(self.fields, h, ldh, y, ldy, g, ldg, pw, pb, w, b, ho, ldho, n, ldn, B._stream(stream)), "mmm_block_norm")
+
+    def launch(self, operands, stream=None) -> None:
+        B._check(B.native.block_norm(self.fields, *operands, B._stream(stream)), "mmm_block_norm")
 
     def backward(self, H_out: Optional[torch.Tensor] = None, grad_normed: Optional[torch.Tensor] = None, grad_H_out: Optional[torch.Tensor] = None,
                  grad_H: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
@@ -110,7 +115,7 @@ class MaskedMlp:
         self.a, self.y = room(M, hidden), room(M, width)
         # what the slope is taken at: ReLU's is told by its value
         self.preact = self.a if activation in (B.MMM_ACT_RELU, B.MMM_ACT_NONE) else room(M, hidden) if training else None
-        self.W1 = self.b1 = self.W2 = self.b2 = None
+        self.W1 = self.b1 = self.W2 = self.b2 = self.built = None   # built: where the N of the last forward call is
         if training:
             self.grad_a, self.grad_y = room(M, hidden), room(M, width)
             nbytes = max(B.mmm_epilogue_backward_workspace_bytes(M, n) for n in (hidden, width))
@@ -143,16 +148,16 @@ class MaskedMlp:
         """H_out may be H (backward() does not need H); normed receives n'."""
         if self.W1 is None:
             raise ValueError("set_weights() comes first")
-        check_device(self.device)
-        places(self.device, 1, ("N",), N, (self.M, self.width), TORCH_TYPES[self.dtype])
+        # (everything is checked before the first launch)
+        norm = self.norm.forward(H, normed, H_out, self.y, gate, post_weight, post_bias, pre_weight, pre_bias, later=True)
+        self.built = places(self.device, 1, ("N",), N, (self.M, self.width), TORCH_TYPES[self.dtype])
         kept = self.preact if self.training and self.preact is not self.a else None
         self.up.build_maps(N, None, stream=stream)
         self.up.matmul_epilogue(N, self.W1, self.a, bias=self.b1, activation=self.activation, preact=kept, stream=stream)
         if not self.fused:
             self.down.build_maps(self.a, None, stream=stream)   # (by the value, not by the sign: NaN has to reach the stream)
         self.down.matmul_epilogue(self.a, self.W2, self.y, bias=self.b2, pred=B.MMM_PRED_NONZERO if self.fused else None, stream=stream)
-        self.norm.forward(H, normed=normed, H_out=H_out, Y=self.y, gate=gate, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight,
-                          pre_bias=pre_bias, stream=stream)
+        self.norm.launch(norm, stream)
 
     def backward(self, N: torch.Tensor, H_out: torch.Tensor, grad_N: torch.Tensor, grad_H: torch.Tensor, grad_normed: Optional[torch.Tensor] = None,
                  grad_H_out: Optional[torch.Tensor] = None, grad_W1: Optional[torch.Tensor] = None, grad_W2: Optional[torch.Tensor] = None,
@@ -163,7 +168,17 @@ class MaskedMlp:
         if not self.training:
             raise ValueError("made without training=True")
         M, ws, od = self.M, self.workspace, self.dtype
-        places(self.device, 0, ("grad_b1", "grad_b2"), grad_b1, (self.hidden,), torch.float32, grad_b2, (self.width,), torch.float32)
+        # (checked before anything is launched, or added to)
+        mk, t, f = (M, self.width), TORCH_TYPES[od], torch.float32
+        at = places(self.device, 1, ("N", "grad_N", "grad_W1", "grad_W2", "grad_b1", "grad_b2"), N, mk, t, grad_N, mk, t, grad_W1, (self.width, self.hidden), f,
+                    grad_W2, (self.hidden, self.width), f, grad_b1, (self.hidden,), f, grad_b2, (self.width,), f)
+        if at[:2] != self.built:
+            raise ValueError("N is not that of a forward call")
+        if grad_N is None and grad_W1 is None:
+            raise ValueError("grad_N or grad_W1 is needed")
+        for name, grad, ld in (("grad_N", grad_N, at[3]), ("grad_W1", grad_W1, at[5]), ("grad_W2", grad_W2, at[7])):
+            if grad is not None and ld < grad.shape[1]:
+                raise ValueError(f"rows of {name} overlap")
         self.norm.backward(H_out=H_out, grad_normed=grad_normed, grad_H_out=grad_H_out, grad_H=grad_H, Y=self.y, grad_Y=self.grad_y, stream=stream, **norm)
         if grad_b2 is not None:
             B.mmm_epilogue_backward(M, self.width, od, od, B.MMM_ACT_NONE, self.grad_y, self.width, None, 0, None, 0, grad_b2, ws, ws.numel(), stream)

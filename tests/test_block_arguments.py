@@ -189,6 +189,7 @@ def mlp_of(calls, M=4, width=16, hidden=32, dtype=mm.MMM_F32, device="cpu", **mo
                         up=Recorder(calls), down=Recorder(calls), norm=mm.BlockNorm(M, width, dtype, mm.MMM_NORM_RMS, device="cpu", training=True),
                         preact=room["a"], W1=torch.zeros(width, hidden, dtype=t), W2=torch.zeros(hidden, width, dtype=t), b1=None, b2=None,
                         workspace=torch.empty(1 << 16, dtype=torch.uint8), **room)
+    mlp.norm.device = mlp.device
     mlp.__dict__.update(more)
     return mlp
 
@@ -204,3 +205,31 @@ def test_the_block_refuses_another_current_device_before_any_launch(monkeypatch)
         with pytest.raises(ValueError, match="current device"):
             call()
     assert calls == []
+
+
+def test_the_block_refuses_operands_before_any_launch(monkeypatch):
+    """A call that cannot be carried out to its end is not begun: with accumulate the weights' gradients have been added to by then."""
+    calls = []
+    mlp = mlp_of(calls, built=None)
+    for name in ("block_norm", "block_norm_backward", "epilogue_backward"):
+        monkeypatch.setattr(B.native, name, lambda *a, name=name: calls.append(name) or 0)
+    monkeypatch.setattr(B, "_stream", lambda s: None)
+    N, w1, w2 = torch.zeros(4, 16), torch.zeros(16, 32), torch.zeros(32, 16)
+    H, out, n = (torch.zeros(4, 16) for _ in range(3))
+    good = dict(N=N, H_out=out, grad_N=torch.zeros(4, 16), grad_H=H, grad_normed=n, grad_W1=w1, grad_W2=w2, grad_b1=torch.zeros(32), accumulate=True)
+    with pytest.raises(ValueError, match="forward"):
+        mlp.backward(**good)                                     # there was none
+    for bad in (dict(H=H[:3]), dict(H_out=out.double()), dict(normed=n[:, :8]), dict(gate=N), dict(pre_weight=N), dict(N=N[:2])):
+        with pytest.raises((ValueError, TypeError)):
+            mlp.forward(**{"N": N, "H": H, "H_out": out, "normed": n, **bad})
+    assert calls == []
+    mlp.forward(N, H, out, n)
+    assert calls == ["build_maps", "matmul_epilogue", "build_maps", "matmul_epilogue", "block_norm"]
+    calls.clear()
+    for bad in (dict(N=N.clone()), dict(N=N[:2]), dict(grad_N=H[:2]), dict(grad_W1=w2), dict(grad_W1=w1.double()), dict(grad_W2=w1), dict(grad_b1=torch.zeros(16)),
+                dict(grad_b2=torch.zeros(32)), dict(grad_N=None, grad_W1=None), dict(grad_W2=torch.zeros(1, 16).expand(32, 16)), dict(grad_H=H[:2])):
+        with pytest.raises((ValueError, TypeError)):
+            mlp.backward(**{**good, **bad})
+    assert calls == []
+    mlp.backward(**good)
+    assert calls == ["block_norm_backward", "matmul_backward", "epilogue_backward", "matmul_backward"]
