@@ -97,6 +97,8 @@ class MaskedMlp:
     def __init__(self, M: int, width: int, hidden: int, block_width: int = 32, dtype: int = B.MMM_BF16, activation: int = B.MMM_ACT_RELU,
                  post: int = B.MMM_NORM_RMS, pre: int = B.MMM_NORM_RMS, gate: int = B.MMM_GATE_NONE, alpha: float = 1.0, eps: float = 1e-5,
                  dtype_h: Optional[int] = None, fused: bool = False, training: bool = False, device="cuda:0"):
+        if dtype not in (B.MMM_F32, B.MMM_BF16, B.MMM_F16):
+            raise ValueError("the norms of the block take floats and 16-bit types")
         if fused and training:
             raise ValueError("the gradients need the maps of the activations, which a fused product does not make")
         if fused and activation != B.MMM_ACT_RELU:

@@ -233,3 +233,10 @@ def test_the_block_refuses_operands_before_any_launch(monkeypatch):
     assert calls == []
     mlp.backward(**good)
     assert calls == ["block_norm_backward", "matmul_backward", "epilogue_backward", "matmul_backward"]
+
+
+@pytest.mark.parametrize("dtype", [mm.MMM_F64, 7])
+def test_the_block_refuses_types_without_norms(dtype):
+    """At once, not behind the products of the first call."""
+    with pytest.raises(ValueError, match="floats"):
+        mm.MaskedMlp(4, 64, 64, dtype=dtype, device="cpu")
