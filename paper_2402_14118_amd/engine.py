@@ -66,7 +66,10 @@ class MaskedMatmul:
                         activation: int = B.MMM_ACT_NONE, residual: Optional[torch.Tensor] = None, preact: Optional[torch.Tensor] = None,
                         pred: Optional[int] = None, threshold: float = 0.0, keep_a: Optional[torch.Tensor] = None, stream=None) -> None:
         """C = activation(A x B + bias) + residual; preact receives A x B + bias.  C, residual and preact are of one type: that of the
-        inputs, or float.  residual may be C.  With a predicate M is evaluated inside the multiplication, as in matmul_fused."""
+        inputs, or float.  residual may be C.  With a predicate M is evaluated inside the multiplication, as in matmul_fused; threshold and
+        keep_a belong to it."""
+        if pred is None and (keep_a is not None or threshold != 0.0):
+            raise ValueError("keep_a and threshold go with a predicate: without one M is that of the maps as built")
         check_device(self.device)
         dt, shape, t, out = self.dtype, (self.M, self.N), TORCH_TYPES[self.dtype], C.dtype
         x, ldx, y, ldy, c, ldc, r, ldr, z, ldp, b, _ = places(

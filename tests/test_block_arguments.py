@@ -240,3 +240,13 @@ def test_the_block_refuses_types_without_norms(dtype):
     """At once, not behind the products of the first call."""
     with pytest.raises(ValueError, match="floats"):
         mm.MaskedMlp(4, 64, 64, dtype=dtype, device="cpu")
+
+
+def test_a_mask_without_a_predicate_is_refused():
+    """Without a predicate the maps say what counts: a mask that is given would be left out."""
+    eng = object.__new__(mm.MaskedMatmul)
+    eng.M, eng.K, eng.N, eng.dtype, eng.device, eng.maps = 4, 8, 16, mm.MMM_BF16, torch.device("cpu"), None
+    X, Y, C = (torch.zeros(s, dtype=torch.bfloat16) for s in ((4, 8), (8, 16), (4, 16)))
+    for mask in (dict(keep_a=torch.zeros(4, 1, dtype=torch.int64)), dict(threshold=0.5)):
+        with pytest.raises(ValueError, match="predicate"):
+            eng.matmul_epilogue(X, Y, C, stream=0, **mask)
