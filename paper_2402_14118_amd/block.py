@@ -11,7 +11,7 @@ import torch
 
 from . import binding as B
 from .engine import MaskedMatmul
-from .tensors import TORCH_TYPES, check_device, own_device, places
+from .tensors import TORCH_TYPES, capturing, check_device, own_device, places
 
 
 class BlockNorm:
@@ -118,6 +118,7 @@ class MaskedMlp:
         # what the slope is taken at: ReLU's is told by its value
         self.preact = self.a if activation in (B.MMM_ACT_RELU, B.MMM_ACT_NONE) else room(M, hidden) if training else None
         self.W1 = self.b1 = self.W2 = self.b2 = self.built = None   # built: where the N of the last forward call is
+        self.counted = False   # and the form of floats has not been chosen since
         if training:
             self.grad_a, self.grad_y = room(M, hidden), room(M, width)
             nbytes = max(B.mmm_epilogue_backward_workspace_bytes(M, n) for n in (hidden, width))
@@ -130,19 +131,24 @@ class MaskedMlp:
     def set_weights(self, W1: torch.Tensor, W2: torch.Tensor, b1: Optional[torch.Tensor] = None, b2: Optional[torch.Tensor] = None,
                     keep_blocks1: Optional[torch.Tensor] = None, keep_blocks2: Optional[torch.Tensor] = None,
                     keep_rows2: Optional[torch.Tensor] = None, stream=None) -> None:
-        """Build the maps of both weights; again after a weight or a selection has changed."""
+        """Build the maps of both weights; again after a weight or a selection has changed.  All of them are kept (see count())."""
         check_device(self.device)
         t = TORCH_TYPES[self.dtype]
         places(self.device, 2, ("W1", "W2", "b1", "b2"), W1, (self.width, self.hidden), t, W2, (self.hidden, self.width), t, b1, (self.hidden,), t, b2, (self.width,), t)
         self.W1, self.W2, self.b1, self.b2 = W1, W2, b1, b2
-        self.up.build_maps(None, W1, keep_blocks=keep_blocks1, stream=stream)
-        self.down.build_maps(None, W2, keep_rows=keep_rows2, keep_blocks=keep_blocks2, stream=stream)
+        self.masks = dict(keep_blocks=keep_blocks1), dict(keep_rows=keep_rows2, keep_blocks=keep_blocks2)
+        self.up.build_maps(None, W1, stream=stream, **self.masks[0])
+        self.down.build_maps(None, W2, stream=stream, **self.masks[1])
 
     def count(self, stream=None):
         """Count the densities of the last forward call (waits for the stream): what the choice of kernel, of tiles and of the form of floats goes by
-        from then on.  Returns ((non-zeros, blocks, products) of the first product, the same of the second; None where its mask is fused)."""
+        from then on.  A side of a product that is built alone keeps the form of the other: the next forward call on floats that is not captured into a
+        graph builds the maps of the weights again, in one with those of its activations.  Returns ((non-zeros, blocks, products) of the first product, the
+        same of the second; None where its mask is fused)."""
         check_device(self.device)
-        return self.up.stats(stream), None if self.fused else self.down.stats(stream)
+        counts = self.up.stats(stream), None if self.fused else self.down.stats(stream)
+        self.counted = self.dtype == B.MMM_F32
+        return counts
 
     def forward(self, N: torch.Tensor, H: torch.Tensor, H_out: torch.Tensor, normed: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
                 post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None, pre_weight: Optional[torch.Tensor] = None,
@@ -154,12 +160,16 @@ class MaskedMlp:
         norm = self.norm.forward(H, normed, H_out, self.y, gate, post_weight, post_bias, pre_weight, pre_bias, later=True)
         self.built = places(self.device, 1, ("N",), N, (self.M, self.width), TORCH_TYPES[self.dtype])
         kept = self.preact if self.training and self.preact is not self.a else None
-        self.up.build_maps(N, None, stream=stream)
+        both = self.counted and not capturing(stream)
+        W1, W2, masks = (self.W1, self.W2, self.masks) if both else (None, None, ({}, {}))
+        self.up.build_maps(N, W1, stream=stream, **masks[0])
         self.up.matmul_epilogue(N, self.W1, self.a, bias=self.b1, activation=self.activation, preact=kept, stream=stream)
         if not self.fused:
-            self.down.build_maps(self.a, None, stream=stream)   # (by the value, not by the sign: NaN has to reach the stream)
+            self.down.build_maps(self.a, W2, stream=stream, **masks[1])   # (by the value, not by the sign: NaN has to reach the stream)
         self.down.matmul_epilogue(self.a, self.W2, self.y, bias=self.b2, pred=B.MMM_PRED_NONZERO if self.fused else None, stream=stream)
         self.norm.launch(norm, stream)
+        if both:
+            self.counted = False
 
     def backward(self, N: torch.Tensor, H_out: torch.Tensor, grad_N: torch.Tensor, grad_H: torch.Tensor, grad_normed: Optional[torch.Tensor] = None,
                  grad_H_out: Optional[torch.Tensor] = None, grad_W1: Optional[torch.Tensor] = None, grad_W2: Optional[torch.Tensor] = None,

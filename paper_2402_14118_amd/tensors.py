@@ -39,3 +39,13 @@ def check_device(device: torch.device) -> None:
     """Kernels are launched on the current device, and on its current stream where none is given."""
     if device.index is not None and device.index != B.current_device() and device.type == "cuda":
         raise ValueError(f"the current device is cuda:{B.current_device()}, the tensors are on {device}")
+
+
+def capturing(stream) -> bool:
+    """Whether work on this stream (a stream, its handle, or None: the current one) goes into a graph."""
+    if isinstance(stream, int):
+        if stream == 0:
+            return False
+        stream = torch.cuda.ExternalStream(stream)
+    with torch.cuda.stream(stream):   # (None: the current one)
+        return torch.cuda.is_current_stream_capturing()

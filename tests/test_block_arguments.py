@@ -187,7 +187,7 @@ def mlp_of(calls, M=4, width=16, hidden=32, dtype=mm.MMM_F32, device="cpu", **mo
     room = {name: torch.zeros(M, n, dtype=t) for name, n in (("a", hidden), ("y", width), ("grad_a", hidden), ("grad_y", width))}
     mlp.__dict__.update(M=M, width=width, hidden=hidden, dtype=dtype, activation=mm.MMM_ACT_RELU, fused=False, training=True, device=torch.device(device),
                         up=Recorder(calls), down=Recorder(calls), norm=mm.BlockNorm(M, width, dtype, mm.MMM_NORM_RMS, device="cpu", training=True),
-                        preact=room["a"], W1=torch.zeros(width, hidden, dtype=t), W2=torch.zeros(hidden, width, dtype=t), b1=None, b2=None,
+                        preact=room["a"], W1=torch.zeros(width, hidden, dtype=t), W2=torch.zeros(hidden, width, dtype=t), b1=None, b2=None, masks=({}, {}), counted=False,
                         workspace=torch.empty(1 << 16, dtype=torch.uint8), **room)
     mlp.norm.device = mlp.device
     mlp.__dict__.update(more)

@@ -172,3 +172,64 @@ def test_two_blocks_at_once():
     torch.cuda.synchronize()
     for want, out in zip(wants, gots):
         assert all(torch.equal(a, b) for pair in out for a, b in zip(want, pair))
+
+
+def whole_block(M=2048, d=2048, f=2048, **how):
+    """A block of floats whose products are exact in any order and form: whole numbers, whose sums stay below 2^24 (|a| <= 9 d + 3, |y| <= (9 d + 3) f, but for
+    signs that do not all agree: counted below)."""
+    g = torch.Generator().manual_seed(2)
+    N, W1, W2 = (torch.randint(-3, 4, s, generator=g).float() for s in ((M, d), (d, f), (f, d)))
+    b1, b2 = torch.randint(-3, 4, (f,), generator=g).float(), torch.randint(-3, 4, (d,), generator=g).float()
+    H = torch.randn(M, d, generator=g)
+    most = torch.relu(N.cuda() @ W1.cuda() + b1.cuda()) @ W2.cuda().abs()
+    assert float(most.max()) < 2 ** 24
+    dev = [v.cuda() for v in (N, W1, W2, b1, b2, H)]
+    keep = words(torch.rand(d, f // 16, generator=g) < 0.4)
+    mlp = mm.MaskedMlp(M, d, f, 16, mm.MMM_F32, **how)
+    mlp.set_weights(*dev[1:5], keep_blocks1=keep)
+    return mlp, dev, keep
+
+
+@pytest.mark.gpu
+def test_the_form_of_floats_follows_the_counts():
+    mlp, (N, W1, W2, b1, b2, H), keep = whole_block()
+    like = mm.MaskedMatmul(2048, 2048, 2048, 16, mm.MMM_F32)
+    like.set_path(mm.MMM_PATH_MATRIX)
+    like.build_maps(N, W1, keep_blocks=keep)
+    like.stats()
+    like.build_maps(N, W1, keep_blocks=keep)
+    chosen = mm.mmm_matmul_form(like.maps)
+    assert chosen == 1               # (where both sides are built with the counts known)
+    outs = [torch.empty_like(H) for _ in range(4)]
+    n = torch.empty_like(H)
+    mlp.forward(N, H, outs[0], n)
+    assert mm.mmm_matmul_form(mlp.up.maps) == 0
+    mlp.count()
+    for out in outs[1:3]:
+        mlp.forward(N, H, out, n)
+        assert mm.mmm_matmul_form(mlp.up.maps) == chosen
+    mlp.set_weights(W1, W2, b1, b2, keep)
+    mlp.forward(N, H, outs[3], n)
+    assert mm.mmm_matmul_form(mlp.up.maps) == chosen
+    assert all(torch.equal(out, outs[0]) for out in outs[1:])
+
+
+@pytest.mark.gpu
+def test_a_captured_block_keeps_the_form_it_has():
+    """Counted and captured before the next call of the program's own: the weights are not built inside the graph, and stay in its form as long as it is there."""
+    mlp, (N, W1, W2, b1, b2, H), _ = whole_block()
+    want, own, out, n = (torch.empty_like(H) for _ in range(4))
+    mlp.forward(N, H, want, n)
+    mlp.count()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mlp.forward(N, H, out, n)
+    for _ in range(3):
+        out.fill_(0.0)
+        own.fill_(0.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        mlp.forward(N, H, own, n)
+        assert mm.mmm_matmul_form(mlp.up.maps) == 0 and torch.equal(own, want)
