@@ -82,11 +82,15 @@ __device__ __forceinline__ double mmm_sigmoid(double v) { return 1.0 / (1.0 + ex
 // e^(x^2) erfc(x) / t is smooth: Q, of degree 8, was fitted to it for u up to 15 (least squares, weighted until the largest relative error was
 // least: 2.0e-8).  Behind that the result is 0 in float.  One path for all lanes: the library's erfc takes both sides of its branches in a wave (777 x 3001 x
 // 1992 half with GELU 17.5 us, with this 16.6; the gradient through GELU, 777 x 1992, 7.7 and 6.1).  Off by up to 8 times 2^-24 of it.
-__device__ __forceinline__ float mmm_normal(float z, float &bell)
+// FINE (results that stay floats): t Q(t) answers a rounding of t with up to 3.7 times as much.  What t is off by, relative to it, is worked out and taken off, and so is what
+// the two products are rounded by: up to 5 times 2^-24, and the 2-norm of GELU's slope over N(-.5, 1) is off by 4.8e-8 instead of 8.7e-8 of it (1024 x 512 x 16384 floats 144.8 -> 147.0 us,
+// 777 x 3001 x 1992 104.6 -> 105.0, gradients the same).
+template <bool FINE> __device__ __forceinline__ float mmm_normal(float z, float &bell)
 {
+    constexpr float S = 0.212132034355964f;   // 0.3 / sqrt 2
     const float u = fminf(fabsf(z), 15.f), square = u * u;
     bell = mmm_exp(-0.5f * square, -0.5f * __builtin_fmaf(u, u, -square));
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(u, 0.212132034355964f, 1.f));   // 0.3 / sqrt 2
+    const float one_and = __builtin_fmaf(u, S, 1.f), t = __builtin_amdgcn_rcpf(one_and);
     float q = -0.0647779107093811f;
     q = __builtin_fmaf(q, t, 0.24286802113056183f);
     q = __builtin_fmaf(q, t, -0.256333589553833f);
@@ -96,19 +100,28 @@ __device__ __forceinline__ float mmm_normal(float z, float &bell)
     q = __builtin_fmaf(q, t, 0.07414324581623077f);
     q = __builtin_fmaf(q, t, 0.08536188304424286f);
     q = __builtin_fmaf(q, t, 0.08459370583295822f);   // (Q / 2)
-    const float tail = bell * t * q;
+    float tail;
+    if constexpr (FINE) {
+        // t (1 + off) is the reciprocal; (t Q)' t / (t Q) is a straight line within .07; products and what they leave
+        const float more = __builtin_fmaf(u, S, -(one_and - 1.f)), off = __builtin_fmaf(-t, more, __builtin_fmaf(-t, one_and, 1.f));
+        const float by = off * __builtin_fmaf(t, 3.9457922f, -0.23464205f);
+        const float tq = t * q, tq_left = __builtin_fmaf(t, q, -tq), all = bell * tq, all_left = __builtin_fmaf(bell, tq, -all);
+        tail = all + __builtin_fmaf(all, by, __builtin_fmaf(bell, tq_left, all_left));
+    } else {
+        tail = bell * t * q;
+    }
     return z < 0.f ? tail : 1.f - tail;
 }
-__device__ __forceinline__ float mmm_normal(float z)
+template <bool FINE> __device__ __forceinline__ float mmm_normal(float z)
 {
     float bell;
-    return mmm_normal(z, bell);
+    return mmm_normal<FINE>(z, bell);
 }
-__device__ __forceinline__ double mmm_normal(double z) { return 0.5 * erfc(z * -0.70710678118654752440); }
+template <bool> __device__ __forceinline__ double mmm_normal(double z) { return 0.5 * erfc(z * -0.70710678118654752440); }
 
 // act(z): GELU is z times the normal distribution function; its tanh form is z times a sigmoid: (1 + tanh u) / 2 = sigmoid(2 u).  An infinite -z is 0 in
-// the limit, where z times 0 is NaN.
-template <typename E, int N> __device__ __forceinline__ void mmm_activate(E (&z)[N], int32_t act)
+// the limit, where z times 0 is NaN.  T: type of the operands.
+template <typename T, typename E, int N> __device__ __forceinline__ void mmm_activate(E (&z)[N], int32_t act)
 {
     if (act == MMM_ACT_RELU) {
 #pragma unroll
@@ -116,7 +129,7 @@ template <typename E, int N> __device__ __forceinline__ void mmm_activate(E (&z)
     } else if (act == MMM_ACT_GELU) {
 #pragma unroll
         for (int q = 0; q < N; ++q) {
-            const E p = mmm_normal(z[q]);
+            const E p = mmm_normal<sizeof(T) == 4>(z[q]);
             z[q] = p == E(0) ? E(0) : z[q] * p;
         }
     } else if (act != MMM_ACT_NONE) {
@@ -128,8 +141,8 @@ template <typename E, int N> __device__ __forceinline__ void mmm_activate(E (&z)
     }
 }
 
-// d[q] *= act'(z[q]); that of ReLU at 0 is 0, at NaN NaN.  The terms with z vanish in both limits.
-template <int N> __device__ __forceinline__ void mmm_apply_slope(float (&d)[N], const float (&z)[N], int32_t act)
+// d[q] *= act'(z[q]); that of ReLU at 0 is 0, at NaN NaN.  The terms with z vanish in both limits.  T: type of the result.
+template <typename T, int N> __device__ __forceinline__ void mmm_apply_slope(float (&d)[N], const float (&z)[N], int32_t act)
 {
     if (act == MMM_ACT_RELU) {
 #pragma unroll
@@ -138,7 +151,7 @@ template <int N> __device__ __forceinline__ void mmm_apply_slope(float (&d)[N], 
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             float bell;
-            const float p = mmm_normal(z[q], bell), more = z[q] * bell * 0.39894228040143267794f;   // 1 / sqrt(2 pi)
+            const float p = mmm_normal<sizeof(T) == 4>(z[q], bell), more = z[q] * bell * 0.39894228040143267794f;   // 1 / sqrt(2 pi)
             d[q] *= fabsf(z[q]) > 15.f ? p : p + more;
         }
     } else if (act != MMM_ACT_NONE) {
@@ -203,7 +216,7 @@ template <typename T, typename E, int N> struct mmm_column_values {
 #pragma unroll
             for (int q = 0; q < N; ++q) z[q] += bias[q];
         if (e.preact != nullptr) store(e.preact, e.ldp, row, col, z);
-        mmm_activate(z, e.activation);
+        mmm_activate<T>(z, e.activation);
     }
     __device__ __forceinline__ void finish(const mmm_epilogue_args &e, E (&z)[N], const E (&more)[N], void *C, int64_t ldc, int64_t row, int64_t col) const
     {

@@ -507,7 +507,7 @@ template <typename T, typename TC> __global__ __launch_bounds__(64 * ACT_WAVES) 
             mmm_load_piece(static_cast<const TC *>(p.dC) + row * p.lddc + col, left, d);
             if (p.activation != MMM_ACT_NONE) {
                 mmm_load_piece(static_cast<const TC *>(p.Z) + row * p.ldz + col, left, z);
-                mmm_apply_slope(d, z, p.activation);
+                mmm_apply_slope<T>(d, z, p.activation);
             }
 #pragma unroll
             for (int q = 0; q < PIECE; ++q) sum[q] += d[q];

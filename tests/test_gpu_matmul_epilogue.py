@@ -237,3 +237,33 @@ def test_another_stream_and_a_replayed_graph(M, path, split):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(C, want) and torch.equal(p.C, want)
+
+
+# Roundings that count, each 2^-24 / sqrt 3 of the result in the mean square at most: GELU the last sum, the bell and the tail; SiLU also a reciprocal; the tanh form
+# also its argument.  Their squares add up.
+@pytest.mark.gpu
+@pytest.mark.parametrize("act,roundings", [("gelu", 3), ("silu", 4), ("gelu_tanh", 5)])
+def test_smooth_activations_of_floats_in_the_mean(act, roundings):
+    """A million arguments of a layer's distribution: activation and slope by the 2-norm, in floats."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    M, N = 1000, 1000
+    z = torch.randn(M, N, generator=g, device="cuda") - 0.5
+    X, Y = torch.zeros(1, 8, device="cuda"), torch.zeros(8, N, device="cuda")
+    C, dZ, ones = torch.empty_like(z), torch.empty_like(z), torch.ones_like(z)
+    # the argument comes in as the bias of a row at a time
+    row = mm.MaskedMatmul(1, 8, N, 8, mm.MMM_F32)
+    row.build_maps(X, Y)
+    for i in range(M):
+        row.matmul_epilogue(X, Y, C[i:i + 1], bias=z[i], activation=ACTS[act])
+    mm.mmm_epilogue_backward(M, N, mm.MMM_F32, mm.MMM_F32, ACTS[act], ones, N, z, N, dZ, N)
+    d = z.double()
+    if act == "gelu":
+        p = 0.5 * torch.erfc(-d / math.sqrt(2))
+        want, slope = d * p, p + d * torch.exp(-0.5 * d * d) / math.sqrt(2 * math.pi)
+    else:
+        inner, inner_slope = (d, 1.0) if act == "silu" else (math.sqrt(8 / math.pi) * (d + 0.044715 * d ** 3), math.sqrt(8 / math.pi) * (1 + 0.134145 * d ** 2))
+        p = torch.sigmoid(inner)
+        want, slope = d * p, p + d * p * torch.sigmoid(-inner) * inner_slope
+    errors = [float((got.double() - w).norm() / w.norm()) for got, w in ((C, want), (dZ, slope))]
+    print(act, errors)
+    assert max(errors) <= math.sqrt(roundings / 3) * U, errors
