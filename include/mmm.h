@@ -444,7 +444,9 @@ mmm_status mmm_block_norm(const mmm_block_norm_desc *desc, const void *h, int64_
                           void *hip_stream);
 
 /* Its gradients.  h_out is the h' of the forward call as stored (h where there was no block; needed with a norm in front, else NULL is allowed), d_n and d_h_out the
- * gradients that come in (d_n must be given exactly where there is a norm in front; d_h_out == NULL: zero, which needs d_n).  Outputs, each optional:
+ * gradients that come in (d_n must be given exactly where there is a norm in front; d_h_out == NULL: zero, which needs d_n).
+ * y says that there was a block, also where no value of it is needed (no norm behind it, no gate): without y there was none, and d_h
+ * is not scaled by alpha, whatever desc->alpha is.  Outputs, each optional:
  *   d_h (dt_h), d_y (dt_y), d_gate (float for MMM_GATE_ROW and MMM_GATE_COL, M x ldd_gate of dt for MMM_GATE_FULL),
  *   d_post_weight, d_post_bias, d_pre_weight, d_pre_bias (N floats each; the values the forward call had may be NULL, i.e. 1 and 0).
  * d_h may be d_h_out itself (same leading dimension).  Sums over rows are float sums in an order that depends on the shape only.

@@ -63,8 +63,9 @@ class BlockNorm:
                  post_bias: Optional[torch.Tensor] = None, pre_weight: Optional[torch.Tensor] = None, grad_post_weight: Optional[torch.Tensor] = None,
                  grad_post_bias: Optional[torch.Tensor] = None, grad_pre_weight: Optional[torch.Tensor] = None,
                  grad_pre_bias: Optional[torch.Tensor] = None, stream=None) -> None:
-        """H_out: as the forward call left it (H where there was no block).  grad_H may be grad_H_out.  Gradients that are not given are
-        not worked out; those of weights, biases and of a gate per row or column are float."""
+        """H_out: as the forward call left it (H where there was no block).  Y: that of the forward call, also where no value of it is needed; without it
+        there was no block, and grad_H is not scaled by alpha.  grad_H may be grad_H_out.  Gradients that are not given are not worked out; those of
+        weights, biases and of a gate per row or column are float."""
         t, th, ty, shape, columns, f = self.type, self.type_h, self.type_y, self.shape, self.columns, torch.float32
         check_device(self.device)
         if self.gate_shape is None and (gate is not None or grad_gate is not None):
