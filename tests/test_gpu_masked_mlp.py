@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2402_14118_amd as mm
+from test_gpu_block_norm import standard as rows_standard
 from test_gpu_matmul_epilogue import T, words
 
 EPS = 1e-5
@@ -233,3 +234,64 @@ def test_a_captured_block_keeps_the_form_it_has():
         assert torch.equal(out, want)
         mlp.forward(N, H, own, n)
         assert mm.mmm_matmul_form(mlp.up.maps) == 0 and torch.equal(own, want)
+
+
+# Each step of the block from what the step before has left in its 16 bits: a result is off by half a step of its type, and by what its own sum of n products in
+# float may be off, (n + 2) * 2^-24 of the magnitudes (norms and their gradients: 160, as derived beside their own tests).
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,act,context", [("bf16", "silu", True), ("bf16", "relu", False), ("f16", "relu", True), ("f16", "silu", False)])
+def test_every_step_of_a_block(dt, act, context):
+    mlp, d, ref, on1, on2 = setup(dt, act, M=70, d=192, f=320, context=context, training=True)
+    M, width, hidden, U = 70, 192, 320, 2.0 ** -24
+    values = {k: d[k] for k in ("gate", "post_weight", "pre_weight")}
+    H_out, n = torch.empty_like(d["H"]), torch.empty_like(d["H"])
+    mlp.forward(d["N"], d["H"], H_out, n, pre_bias=d["pre_bias"], **values)
+    r = {k: v.detach() for k, v in ref.items()}
+    half, tiny = torch.finfo(d["N"].dtype).eps / 2, torch.finfo(d["N"].dtype).smallest_normal * torch.finfo(d["N"].dtype).eps
+
+    def of(t):
+        return t.double().cpu()
+
+    def step(what, got, want, mag, roundings=1):
+        steps = 0.0 if got.dtype == torch.float32 else half * roundings * (1 + half)
+        bound = steps * want.abs() + mag * U * (1 + 2 * half) + tiny
+        err = (of(got) - want).abs()
+        assert bool((err <= bound).all()), (what, float((err / bound).max()))
+    W1, W2 = r["W1"] * on1, r["W2"] * on2
+    # forward; an activation has a slope of 1.13 at most, and errs by 16 roundings of 1 + |z|
+    z, mag = r["N"] @ W1 + r["b1"], (width + 2) * (r["N"].abs() @ W1.abs() + r["b1"].abs())
+    step("a", mlp.a, torch.relu(z) if act == "relu" else z * torch.sigmoid(z), 1.13 * mag + 16 * (1 + z.abs()))
+    if act != "relu":
+        step("preact", mlp.preact, z, mag)
+    a = of(mlp.a)
+    step("y", mlp.y, a @ W2 + r["b2"], (hidden + 2) * (a.abs() @ W2.abs() + r["b2"].abs()))
+    y = of(mlp.y)
+    zy, mzy, ry = rows_standard(y, "rms")
+    h, mh = 0.9 * r["H"] + r["gate"] * zy * r["post_weight"], 0.9 * r["H"].abs() + (r["gate"] * r["post_weight"]).abs() * mzy
+    step("H_out", H_out, h, 160 * mh)
+    zh, mzh, rh = rows_standard(h, "layer")
+    extra = mh * rh + mh.mean(1, keepdim=True) * rh + zh.abs() * ((zh.abs() * mh).mean(1, keepdim=True) * rh)
+    step("n", n, zh * r["pre_weight"] + r["pre_bias"], 160 * ((mzh + extra) * r["pre_weight"].abs() + r["pre_bias"].abs()))
+    # backward
+    g = torch.Generator().manual_seed(8)
+    up_n, up_h = (torch.randn(M, width, generator=g).to(T[dt][1]) for _ in range(2))
+    out = {"grad_N": torch.empty_like(d["N"]), "grad_H": torch.empty_like(d["H"]), **{"grad_" + k: torch.full(d[k].shape, float("nan"), device="cuda") for k in ("W1", "W2", "b1", "b2")}}
+    mlp.backward(d["N"], H_out, grad_normed=up_n.cuda(), grad_H_out=up_h.cuda(), **values, **out)
+    x, mx, rx = rows_standard(of(H_out), "layer")
+    u, dh = of(up_n) * r["pre_weight"], of(up_h)
+    dh, mdh = (dh + rx * (u - x * (u * x).mean(1, keepdim=True) - u.mean(1, keepdim=True)),
+               dh.abs() + rx * (u.abs() + mx * (u.abs() * mx).mean(1, keepdim=True) + u.abs().mean(1, keepdim=True)))
+    step("grad_H", out["grad_H"], 0.9 * dh, 160 * 0.9 * mdh)
+    u, mu = dh * r["gate"] * r["post_weight"], mdh * (r["gate"] * r["post_weight"]).abs()
+    step("grad_y", mlp.grad_y, ry * (u - zy * (u * zy).mean(1, keepdim=True)), 160 * ry * (mu + mzy * (mu * mzy).mean(1, keepdim=True)))
+    dy = of(mlp.grad_y)
+    step("grad_b2", out["grad_b2"], dy.sum(0), M * dy.abs().sum(0))
+    step("grad_W2", out["grad_W2"], a.t() @ dy * on2, (M + 2) * (a.abs().t() @ dy.abs()) * on2)
+    at = of(mlp.preact)
+    slope = (at > 0).double() if act == "relu" else torch.sigmoid(at) * (1 + at * torch.sigmoid(-at))
+    da, mda = dy @ W2.t(), (width + 2) * (dy.abs() @ W2.abs().t())
+    step("grad_z", mlp.grad_a, da * slope, (mda + 16 * da.abs()) * (1.13 if act != "relu" else 1.0), roundings=2)   # (the product's, and behind the slope)
+    dz = of(mlp.grad_a)
+    step("grad_b1", out["grad_b1"], dz.sum(0), (M + half / U * (1 + 2 * half)) * dz.abs().sum(0))              # (summed before it is rounded)
+    step("grad_W1", out["grad_W1"], r["N"].t() @ dz * on1, (M + 2) * (r["N"].abs().t() @ dz.abs()) * on1)
+    step("grad_N", out["grad_N"], dz @ W1.t(), (hidden + 2) * (dz.abs() @ W1.abs().t()))

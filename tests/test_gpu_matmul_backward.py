@@ -312,3 +312,32 @@ def test_a_captured_gradient_fixes_the_form(form):
             p.check(exact=True)
     finally:
         mm.mmm_set_option("float_form", -1)
+
+
+TILES = [("bf16", 1000, 4100, 2080, None), ("f16", 2048, 2048, 1032, 0.5), ("f32", 1300, 2300, 1544, None), ("f32", 2050, 3000, 1032, 0.4), ("bf16", 2900, 5000, 4104, None),
+         ("bf16", 24, 70, 8192, None), ("f32", 2048, 72, 136, None), ("f16", 2000, 130, 64, 0.5), ("bf16", 2051, 2055, 72, 0.1), ("f16", 4001, 1153, 136, 0.5),
+         ("bf16", 1030, 8200, 520, 0.5), ("f16", 2051, 16391, 1032, 0.9), ("f32", 777, 3001, 1992, 0.25)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,M,K,N,rows", TILES)
+def test_whole_numbers_in_every_tile(dt, M, K, N, rows):
+    """All tiles, parts and ways of storing, with whole numbers from -3 to 3: sums are exact (9 * 8192 < 2^24), so a product that is lost or counted twice shows."""
+    g = torch.Generator(device="cuda").manual_seed(M + K + N)
+    t = T[dt][1]
+    X, Y, dC = (torch.randint(-3, 4, s, generator=g, device="cuda").to(t) for s in ((M, K), (K, N), (M, N)))
+    keep = torch.rand(M, K, generator=g, device="cuda") < 0.6
+    blocks = torch.rand(K, N // 8, generator=g, device="cuda") < 0.7
+    on = torch.ones(K, dtype=torch.bool, device="cuda") if rows is None else torch.rand(K, generator=g, device="cuda") < rows
+    eng = mm.MaskedMatmul(M, K, N, 8, T[dt][0])
+    eng.build_maps(X, Y, keep_a=words(keep.cpu()), keep_rows=None if rows is None else words(on.view(1, -1).cpu()), keep_blocks=words(blocks.cpu()))
+    A, Bm, G = X.double() * keep, Y.double() * (blocks & on.view(-1, 1)).repeat_interleave(8, 1), dC.double()
+    all_dx, want_y = G @ Bm.t().contiguous(), (A.t().contiguous() @ G) * (Bm.view(K, -1, 8) != 0).any(2).repeat_interleave(8, 1)
+    for counted in (False, True):
+        if counted:
+            eng.stats()
+        dX, dY = torch.full_like(X, 7.0), torch.full((K, N), 7.0, device="cuda")
+        eng.matmul_backward(X, Y, dC, dX, dY)
+        assert torch.equal(dX, (all_dx * (A != 0)).to(t)) and torch.equal(dY.double(), want_y), counted
+        eng.matmul_backward(X, Y, dC, dX, all_x=True)
+        assert torch.equal(dX, all_dx.to(t)), counted

@@ -267,3 +267,34 @@ def test_smooth_activations_of_floats_in_the_mean(act, roundings):
     errors = [float((got.double() - w).norm() / w.norm()) for got, w in ((C, want), (dZ, slope))]
     print(act, errors)
     assert max(errors) <= math.sqrt(roundings / 3) * U, errors
+
+
+@pytest.mark.gpu
+def test_columns_left_out_are_not_multiplied():
+    """What rows of Y hold whose column of A is zero in a whole tile: a kernel that multiplied them by their zeros would bring NaN."""
+    M, K, N = 128, 2048, 512
+    g = torch.Generator(device="cuda").manual_seed(1)
+    X, Y = torch.randn(M, K, generator=g, device="cuda"), torch.randn(K, N, generator=g, device="cuda")
+    X[:, torch.arange(K, device="cuda") % 9 != 0] = 0.0
+    bias, R = torch.randn(N, generator=g, device="cuda"), torch.randn(M, N, generator=g, device="cuda")
+    dirty = Y.clone()
+    dirty[torch.arange(K, device="cuda") % 9 != 0, ::3] = float("nan")
+    eng = mm.MaskedMatmul(M, K, N, 16, mm.MMM_F32)
+    eng.set_path(mm.MMM_PATH_MATRIX)
+    eng.build_maps(X, Y)
+    eng.stats()
+    tiles = []
+    for v in range(mm.mmm_matmul_variant_count()):
+        eng.set_plan(v, 1)
+        if eng.plan()[:2] != (v, 1):
+            continue
+        outs = []
+        for right in (Y, dirty):
+            eng.build_maps(X, right)
+            assert mm.mmm_matmul_form(eng.maps) == 0
+            C = torch.empty(M, N, device="cuda")
+            eng.matmul_epilogue(X, right, C, bias=bias, activation=ACTS["relu"], residual=R)
+            outs.append(C)
+        assert bool(outs[0].isfinite().all()) and torch.equal(*outs), v
+        tiles.append(v)
+    assert tiles == [0, 1, 2, 6, 7]

@@ -104,3 +104,24 @@ def test_groups_that_a_wave_walks(tmp_path):
 def test_blocks_of_a_over_the_workgroups(tmp_path):
     """Every block once, and as many for each XCD, also where the last row of workgroups has fewer blocks than the others."""
     assert _printed(tmp_path, PLACES) == "0"
+
+
+@pytest.mark.parametrize("N,bw", [(264, 8), (288, 16), (288, 32)])
+@pytest.mark.parametrize("dtype", [mm.MMM_F32, mm.MMM_BF16, mm.MMM_F16, mm.MMM_F64])
+@pytest.mark.parametrize("M", [30, 130])
+def test_plans_that_can_be_fixed(M, dtype, N, bw):
+    """Every tile with K in one part and in three, as comparisons of all of them go through: 32-row tiles are for at most 32 rows, two ranges of K not for doubles."""
+    need = mm.mmm_maps_workspace_bytes_for(M, 700, N, bw, dtype)
+    maps = mm.mmm_maps_init(0x7000_0000_0000, need, M, 700, N, bw)
+    try:
+        mm.mmm_maps_set_path(maps, mm.MMM_PATH_MATRIX)
+        taken = []
+        for v in range(mm.mmm_matmul_variant_count()):
+            for split in (1, 3):
+                mm.mmm_maps_set_plan(maps, v, split)
+                if mm.mmm_matmul_plan(maps, dtype)[:2] == (v, split):
+                    taken.append((v, split))
+        tiles = [v for v in range(8) if (M <= 32 or v not in (3, 4, 5)) and (dtype != mm.MMM_F64 or v not in (4, 6, 7))]
+        assert taken == [(v, split) for v in tiles for split in (1, 3)]
+    finally:
+        mm.mmm_maps_release(maps)
