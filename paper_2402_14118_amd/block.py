@@ -89,7 +89,7 @@ class MaskedMlp:
 
     W1 (width x hidden) and W2 (hidden x width) are masked in blocks of their rows (a block that holds only zeros is off, and learns nothing); rows of W2 (hidden units) may be selected by context.  The
     holder owns the maps of both products, the activations between them and, with training=True, the gradients on the way and the
-    workspaces of backward(): two calls that may run at the same time need a holder each.  fused (few rows of ReLU activations, not for
+    workspaces of backward(): two calls that may run at the same time need a holder each.  y and the gradients on the way have the type of the weights.  fused (few rows of ReLU activations, not for
     training): the second product evaluates their mask itself, in one launch.
 
     A dense operand is multiplied by the matrix kernel (4 x 4096 x 16384 bf16, all blocks on: 29 us with its build, 109 by the pair kernel); for
