@@ -404,6 +404,8 @@ mmm_status mmm_epilogue_backward(int64_t M, int64_t N, mmm_dtype dt, mmm_dtype o
  * like others, where the mask only saves work); a block of weights has to start from something.  X, Y, dC (M x lddc) and dX have type dt; dY is float. dX or dY may
  * be NULL (not both).  accumulate != 0: dY += instead (unoccupied blocks stay as they are).  dX and dY overlap no input.
  * X must be the one the A side was built from (address, ldx); the Y given is what is read, under the maps as built.
+ * A call that is captured into a graph works over the live rows or over all, as the B side was built then (mmm_maps_view_compacted): replays may follow other
+ * selections of rows, but not a build that goes from one of the two to the other.
  * Masked-out elements of X and unoccupied blocks of Y never reach the arithmetic, whatever they hold.  Elements of dC are expected
  * to be finite: one that is not makes row i of dX and column j of dY non-finite, or less than that.
  * Sums in float, in an order that depends on the shape, lddc, the form of the maps and the counts of mmm_maps_stats only

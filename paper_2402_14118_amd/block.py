@@ -132,7 +132,8 @@ class MaskedMlp:
     def set_weights(self, W1: torch.Tensor, W2: torch.Tensor, b1: Optional[torch.Tensor] = None, b2: Optional[torch.Tensor] = None,
                     keep_blocks1: Optional[torch.Tensor] = None, keep_blocks2: Optional[torch.Tensor] = None,
                     keep_rows2: Optional[torch.Tensor] = None, stream=None) -> None:
-        """Build the maps of both weights; again after a weight or a selection has changed.  All of them are kept (see count())."""
+        """Build the maps of both weights; again after a weight or a selection has changed.  All of them are kept (see count()).
+        Where calls have been captured into a graph, keep_rows2 is given from then on exactly if it was then."""
         check_device(self.device)
         t = TORCH_TYPES[self.dtype]
         places(self.device, 2, ("W1", "W2", "b1", "b2"), W1, (self.width, self.hidden), t, W2, (self.hidden, self.width), t, b1, (self.hidden,), t, b2, (self.width,), t)
